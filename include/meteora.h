@@ -344,6 +344,164 @@ int meteora_describe_plan(const meteora_shape_t* shape, char* buf, size_t buf_by
  */
 int meteora_set_tuning(const char* name, int value);
 
+/*
+ * What stands between the q/k/v linears and the o linear of a decoder layer: rotary positions, norms of the query and key
+ * heads, a paged cache of keys and values, and attention for a batch whose sequences share a prefix.  (The paper has no
+ * counterpart: its method replaces the linears of a block and leaves these as they are, Sec. 3.1.)
+ *
+ * Conventions of these calls, next to those at the top of this file
+ *   - Tensors of heads are x[T, heads, head_dim] with element strides of their own for tokens and heads (a slice of a
+ *     fused q/k/v product needs no copy); the entries of a head are contiguous.  1 <= head_dim <= METEORA_MAX_HEAD_DIM.
+ *     Base pointers need the alignment of their element type; 16-byte aligned bases and strides take the wider loads.
+ *   - An output may be its own input (same pointer and strides); any other overlap of tensors is out of contract, and
+ *     an output whose strides make two of its entries coincide is refused.
+ *   - bf16 results are rounded once, from fp32.  `stream` belongs to the device that is current.
+ *   - The calls keep no state: calls on different streams need different workspaces and nothing else.
+ */
+#define METEORA_MAX_HEAD_DIM 256
+#define METEORA_MAX_BATCH 4096 /* sequences of a batch over a paged cache */
+
+typedef enum { METEORA_ROTARY_HALF = 0, METEORA_ROTARY_INTERLEAVED = 1 } meteora_rotary_layout_t;
+typedef enum { METEORA_ROTARY_NONE = 0, METEORA_ROTARY_LINEAR = 1, METEORA_ROTARY_BANDS = 2 } meteora_rotary_scaling_t;
+
+/*
+ * A rotary embedding: the first `dim` entries of a head are dim/2 pairs, pair i turned by position * f_i with
+ * f_i = theta^(-2i/dim), the rest of the head passes through.  Pair i is entries (i, i + dim/2) in the half layout and
+ * (2i, 2i + 1) in the interleaved one:
+ *     (a, b) -> attention_scale * (a cos - b sin, b cos + a sin).
+ * Scaling for contexts longer than the trained one:
+ *   LINEAR  f_i / factor (positions interpolated)
+ *   BANDS   g f_i + (1 - g) f_i / factor with g = (original_context / wavelength_i - low) / (high - low), clamped to
+ *           [0, 1], wavelength_i = 2 pi / f_i: fast pairs keep their frequency, slow ones are interpolated.
+ */
+typedef struct {
+    int dim;                 /* rotated entries of a head: even, 2 <= dim <= METEORA_MAX_HEAD_DIM */
+    meteora_rotary_layout_t layout;
+    double theta;            /* > 0 */
+    meteora_rotary_scaling_t scaling;
+    double factor;           /* > 0; LINEAR and BANDS */
+    double original_context; /* > 0; BANDS */
+    double low, high;        /* low < high; BANDS */
+    float attention_scale;   /* multiplies the rotated entries; 1.0f = a plain rotation */
+} meteora_rotary_spec_t;
+
+/*
+ * The embedding as the kernels take it (plain host memory, copied into each launch).  turns[i] is f_i / (2 pi) in units
+ * of 2^-64 turns: a position times it, modulo 2^64, is the angle modulo a turn, exact for any int64 position up to the
+ * 2^-65 that the frequency was rounded by, so angles of far positions lose nothing.
+ */
+typedef struct {
+    uint64_t turns[METEORA_MAX_HEAD_DIM / 2];
+    int32_t dim, layout;
+    float scale;
+    int32_t reserved;
+} meteora_rotary_t;
+
+/* Fills *rot from *spec.  Host only. */
+int meteora_rotary_init(const meteora_rotary_spec_t* spec, meteora_rotary_t* rot);
+
+typedef struct {
+    void* data;
+    int64_t stride_token, stride_head; /* in elements */
+    int heads;
+} meteora_heads_t;
+
+/*
+ * Rotates query and key heads in one launch: q_out = R(q), k_out = R(k).  k and k_out may both be NULL (one tensor).
+ * positions[T]: int64 where positions_64 is not 0, else int32; any value, negative ones turn backwards.
+ * inverse != 0 turns by the negative angles, with the same scale: the gradient (dq, dk) from (dq_out, dk_out).
+ */
+int meteora_rotary(const meteora_heads_t* q, const meteora_heads_t* k, const meteora_heads_t* q_out,
+                   const meteora_heads_t* k_out, const void* positions, int positions_64, int T, int head_dim,
+                   meteora_dtype_t dtype, const meteora_rotary_t* rot, int inverse, void* stream);
+
+/*
+ * Norm of every query and key head, then the rotation, in one pass:
+ *     y = R(x * r * gain),  r = 1 / sqrt(mean(x^2) + eps) over the head's entries.
+ * q_gain, k_gain: [head_dim] in dtype, shared by the heads of their tensor.  rot may be NULL (norm alone).  eps >= 0;
+ * with eps = 0 a head of zeros has no direction and gives NaN.
+ */
+int meteora_head_norm_rotary(const meteora_heads_t* q, const meteora_heads_t* k, const void* q_gain, const void* k_gain,
+                             const meteora_heads_t* q_out, const meteora_heads_t* k_out, const void* positions,
+                             int positions_64, int T, int head_dim, meteora_dtype_t dtype, const meteora_rotary_t* rot,
+                             float eps, void* stream);
+
+/*
+ * Its gradients, from the forward's inputs (nothing else is kept).  With dn = R^T(dy), n = x * r:
+ *     dx = r * (gain * dn - n * mean(gain * dn * n)),   dgain = sum over tokens and heads of dn * n.
+ * dq_out, dk_out: gradients of the outputs; dq, dk: of the inputs, in dtype; dq_gain, dk_gain: fp32 [head_dim],
+ * overwritten, summed in a fixed order (bit-identical from run to run).  T = 0 gives zero gains.
+ * workspace: meteora_head_norm_rotary_backward_workspace_bytes(T, ...) bytes, no initial contents needed.
+ */
+size_t meteora_head_norm_rotary_backward_workspace_bytes(int T, int q_heads, int k_heads, int head_dim);
+int meteora_head_norm_rotary_backward(const meteora_heads_t* dq_out, const meteora_heads_t* dk_out,
+                                      const meteora_heads_t* q, const meteora_heads_t* k, const void* q_gain,
+                                      const void* k_gain, const meteora_heads_t* dq, const meteora_heads_t* dk,
+                                      float* dq_gain, float* dk_gain, const void* positions, int positions_64, int T,
+                                      int head_dim, meteora_dtype_t dtype, const meteora_rotary_t* rot, float eps,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Keys and values in pages: k and v are [n_pages, kv_heads, page_size, head_dim], contiguous, 16-byte aligned. */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t n_pages;
+    int kv_heads, page_size, head_dim;
+    meteora_dtype_t dtype;
+} meteora_cache_t;
+
+/*
+ * B sequences and their T new tokens.  Token t belongs to the sequence b with cu_tokens[b] <= t < cu_tokens[b + 1];
+ * cu_tokens may be NULL where every sequence has one (T == B).  All sequences start with the same `prefix_len` tokens,
+ * held in prefix_pages (the last page may be partly used); sequence b's own tokens follow in the pages page_table[b],
+ * lengths[b] of them in the cache BEFORE this step's.  The j-th new token of sequence b is its own token
+ * i = lengths[b] + j, at position prefix_len + i, in entry i % page_size of page page_table[b][i / page_size].
+ *   - lengths[b] < 0 marks b as padding: it has no tokens.  So have t < cu_tokens[0] and t >= cu_tokens[B] no sequence.
+ *   - A page number outside [0, n_pages), or an i past the table, is a place that does not exist: nothing is written
+ *     there, and attention does not see it (a page that has been dropped).
+ *   - cu_tokens has to ascend.  Numbers are checked on the device: wrong ones change results, not other memory.
+ * The same batch describes a step's append and its attention; lengths grow afterwards.
+ */
+typedef struct {
+    int B, T;
+    const int32_t* cu_tokens;    /* [B + 1] or NULL */
+    const int32_t* lengths;      /* [B] */
+    const int32_t* page_table;   /* [B, table_width] */
+    int table_width;
+    int prefix_len;              /* tokens of the shared prefix, >= 0 */
+    const int32_t* prefix_pages; /* [ceil(prefix_len / page_size)]; read by attention alone */
+} meteora_batch_t;
+
+/*
+ * Appends the new tokens' keys and values to the cache, with the norm (k_gain != NULL) and the rotation (rot != NULL)
+ * applied to the keys on the way, in one launch; with q the query heads are normed and rotated too (q_out).  v is
+ * copied bit for bit.  Tokens without a sequence or a place are skipped (their q_out rows too where they have no
+ * sequence).  Two tokens with the same place (a page that two sequences both write) are out of contract: which one
+ * stays is not defined.
+ */
+int meteora_cache_append(const meteora_heads_t* k, const meteora_heads_t* v, const meteora_heads_t* q,
+                         const meteora_heads_t* q_out, const void* q_gain, const void* k_gain, float eps,
+                         const meteora_rotary_t* rot, const meteora_cache_t* cache, const meteora_batch_t* batch,
+                         void* stream);
+
+/*
+ * Attention of the batch's new tokens: row (t, h) is the average of values weighted by softmax(scale * q . k) over the
+ * prefix and the own tokens up to its own (i <= lengths[b] + j), query head h reading kv head h / (q heads / kv heads).
+ * The prefix is computed once for the rows of all sequences together; each sequence's own pages for its own rows.
+ *   q, out     [T, q_heads, head_dim] in the cache's dtype; q_heads a multiple of kv_heads.  A row that sees no key at
+ *              all (every page dropped) is zero.  Rows of tokens without a sequence are left as they were.
+ *   lse        optional fp32 [T, q_heads]: logarithm of the row's sum of exp(scale * q . k), -inf for a row that sees none.
+ *   workspace  meteora_prefix_attention_workspace_bytes(...) bytes (sizes of cache and batch are read, no pointers), 16-byte
+ *              aligned, its header zeroed once (meteora_workspace_init); meteora_workspace_status reads its status word.
+ * table_width * page_size and prefix_len stay below 2^29.  Scores, weights' sums and the output are held in fp32; on
+ * bf16 caches the weights are rounded to bf16 for the product with the values and enter their sum rounded alike.
+ * A value that is no finite number reaches the rows that see its token and no others.
+ */
+size_t meteora_prefix_attention_workspace_bytes(const meteora_cache_t* cache, const meteora_batch_t* batch, int q_heads);
+int meteora_prefix_attention(const meteora_heads_t* q, const meteora_cache_t* cache, const meteora_batch_t* batch,
+                             float scale, const meteora_heads_t* out, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
 const char* meteora_status_string(int status);
 
 #ifdef __cplusplus

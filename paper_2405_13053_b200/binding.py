@@ -30,12 +30,48 @@ EXPORTS = ["meteora_gate_topk", "meteora_route", "meteora_lora_delta", "meteora_
            "meteora_adapters_bt_bytes", "meteora_pad_adapters", "meteora_pad_adapters_bytes",
            "meteora_linear_forward_host", "meteora_workspace_bytes", "meteora_workspace_routing",
            "meteora_workspace_init", "meteora_workspace_status", "meteora_profile_begin", "meteora_profile_end",
-           "meteora_describe_plan", "meteora_set_tuning", "meteora_status_string"]
+           "meteora_describe_plan", "meteora_set_tuning", "meteora_status_string",
+           "meteora_rotary_init", "meteora_rotary", "meteora_head_norm_rotary",
+           "meteora_head_norm_rotary_backward_workspace_bytes", "meteora_head_norm_rotary_backward", "meteora_cache_append",
+           "meteora_prefix_attention_workspace_bytes", "meteora_prefix_attention"]
 
 
 class MeteoraShape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int), ("d_in", ctypes.c_int), ("d_out", ctypes.c_int), ("N", ctypes.c_int),
                 ("r", ctypes.c_int), ("k", ctypes.c_int), ("dtype", ctypes.c_int), ("temperature", ctypes.c_float)]
+
+
+MAX_HEAD_DIM, MAX_BATCH = 256, 4096
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "bands": 2}
+
+
+class MeteoraRotarySpec(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int), ("layout", ctypes.c_int), ("theta", ctypes.c_double), ("scaling", ctypes.c_int),
+                ("factor", ctypes.c_double), ("original_context", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("attention_scale", ctypes.c_float)]
+
+
+class MeteoraRotary(ctypes.Structure):
+    """A rotary embedding as the calls take it (host memory, copied into each launch); made by meteora_rotary_init."""
+    _fields_ = [("turns", ctypes.c_uint64 * (MAX_HEAD_DIM // 2)), ("dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class MeteoraHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("heads", ctypes.c_int)]
+
+
+class MeteoraCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class MeteoraBatch(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("cu_tokens", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("table_width", ctypes.c_int), ("prefix_len", ctypes.c_int),
+                ("prefix_pages", ctypes.c_void_p)]
 
 
 class MeteoraError(RuntimeError):
@@ -91,8 +127,22 @@ def load_library() -> ctypes.CDLL:
     lib.meteora_set_tuning.argtypes = [ctypes.c_char_p, ci]
     lib.meteora_status_string.argtypes = [ci]
     lib.meteora_status_string.restype = ctypes.c_char_p
+    heads, rot = ctypes.POINTER(MeteoraHeads), ctypes.POINTER(MeteoraRotary)
+    cache, batch, cf = ctypes.POINTER(MeteoraCache), ctypes.POINTER(MeteoraBatch), ctypes.c_float
+    lib.meteora_rotary_init.argtypes = [ctypes.POINTER(MeteoraRotarySpec), rot]
+    lib.meteora_rotary.argtypes = [heads, heads, heads, heads, vp, ci, ci, ci, ci, rot, ci, vp]
+    lib.meteora_head_norm_rotary.argtypes = [heads, heads, vp, vp, heads, heads, vp, ci, ci, ci, ci, rot, cf, vp]
+    lib.meteora_head_norm_rotary_backward_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.meteora_head_norm_rotary_backward_workspace_bytes.restype = sz
+    lib.meteora_head_norm_rotary_backward.argtypes = [heads, heads, heads, heads, vp, vp, heads, heads, vp, vp, vp, ci, ci,
+                                                      ci, ci, rot, cf, vp, sz, vp]
+    lib.meteora_cache_append.argtypes = [heads, heads, heads, heads, vp, vp, cf, rot, cache, batch, vp]
+    lib.meteora_prefix_attention_workspace_bytes.argtypes = [cache, batch, ci]
+    lib.meteora_prefix_attention_workspace_bytes.restype = sz
+    lib.meteora_prefix_attention.argtypes = [heads, cache, batch, cf, heads, vp, vp, sz, vp]
     for name in EXPORTS:
-        if name not in ("meteora_workspace_bytes", "meteora_group_workspace_bytes",
+        if name not in ("meteora_prefix_attention_workspace_bytes", "meteora_head_norm_rotary_backward_workspace_bytes",
+                        "meteora_workspace_bytes", "meteora_group_workspace_bytes",
                         "meteora_gate_backward_workspace_bytes", "meteora_gate_backward_bt", "meteora_transpose_adapters_b",
            "meteora_adapters_bt_bytes", "meteora_pad_adapters", "meteora_pad_adapters_bytes", "meteora_status_string"):
             getattr(lib, name).restype = ci
@@ -248,6 +298,76 @@ def meteora_linear_forward_host(x_host, W0, A, B, Wg, k: int, y_host: torch.Tens
                                 temperature: float = 1.0) -> torch.Tensor:
     """x_host / y_host are (pinned) host tensors; weights and workspace are CUDA tensors.  Asynchronous."""
     return (_native or _load_native()).linear_forward_host(x_host, W0, A, B, Wg, k, y_host, workspace, temperature)
+
+
+def meteora_rotary_init(dim: int, theta: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                        original_context: float = 0.0, low: float = 1.0, high: float = 4.0,
+                        attention_scale: float = 1.0) -> MeteoraRotary:
+    """A rotary embedding of the first `dim` entries of a head: pairs (i, i + dim/2) ("half") or (2i, 2i + 1)
+    ("interleaved"), frequencies theta^(-2i/dim), scaled for long contexts by "linear" (divided by `factor`) or "bands"
+    (slow pairs divided, fast ones kept; include/meteora.h has the formula).  Made once; host only."""
+    if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"layout is one of {list(ROTARY_LAYOUTS)}, scaling one of {list(ROTARY_SCALINGS)}")
+    spec = MeteoraRotarySpec(int(dim), ROTARY_LAYOUTS[layout], float(theta), ROTARY_SCALINGS[scaling], float(factor),
+                             float(original_context), float(low), float(high), float(attention_scale))
+    rot = MeteoraRotary()
+    _check(load_library().meteora_rotary_init(ctypes.byref(spec), ctypes.byref(rot)), "meteora_rotary_init")
+    return rot
+
+
+def meteora_rotary(q, k, positions, rot: MeteoraRotary, inverse: bool = False, out_q=None, out_k=None):
+    """(q', k'): query heads [T, heads, dim] and key heads (or None) turned by their positions [T] (int32 or int64).  Strides
+    of tokens and heads are free.  `inverse` turns back: the gradient of (q, k) from that of (q', k').  out_q, out_k may
+    be q, k themselves."""
+    return (_native or _load_native()).rotary(q, k, positions, rot, inverse, out_q, out_k)
+
+
+def meteora_head_norm_rotary(q, k, q_gain, k_gain, positions, rot: Optional[MeteoraRotary], eps: float = 1e-5, out_q=None,
+                             out_k=None):
+    """(q', k'): every head divided by its root mean square, times its tensor's gain [dim], then turned (rot None: not).
+    k, k_gain may be None."""
+    return (_native or _load_native()).head_norm_rotary(q, k, q_gain, k_gain, positions, rot, eps, out_q, out_k)
+
+
+def meteora_head_norm_rotary_backward(dq, dk, q, k, q_gain, k_gain, positions, rot: Optional[MeteoraRotary], eps: float = 1e-5,
+                                      workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dq_gain, dk_gain) of meteora_head_norm_rotary from the gradients of its results and its inputs; the
+    gains' gradients are fp32 [dim], summed in a fixed order."""
+    return (_native or _load_native()).head_norm_rotary_backward(dq, dk, q, k, q_gain, k_gain, positions, rot, eps, workspace)
+
+
+def meteora_cache_append(k, v, k_cache, v_cache, page_table, lengths, rot: Optional[MeteoraRotary], cu_tokens=None,
+                         prefix_len: int = 0, q=None, q_gain=None, k_gain=None, eps: float = 1e-5, out_q=None):
+    """Writes the new tokens' keys (normed where k_gain is given, turned where rot is) and values [T, kv heads, dim] into the
+    pages [pages, kv heads, page size, dim] of their sequences; with q, returns the query heads normed and turned alike.
+    lengths[B] int32: tokens each sequence has in the cache before this call, negative for padding (not changed here);
+    cu_tokens[B + 1] int32: first new token of each, None where every sequence has one."""
+    return (_native or _load_native()).cache_append(k, v, k_cache, v_cache, page_table, lengths, rot, cu_tokens, prefix_len, q,
+                                                    q_gain, k_gain, eps, out_q)
+
+
+def meteora_prefix_attention_workspace(q, k_cache, page_table, prefix_len: int = 0) -> torch.Tensor:
+    """Scratch for meteora_prefix_attention calls of these sizes (header zeroed); one per stream."""
+    T, H, _ = q.shape
+    n, kv, page, D = k_cache.shape
+    cache = MeteoraCache(None, None, n, kv, page, D, _dtype_code(k_cache))
+    batch = MeteoraBatch(page_table.shape[0], T, None, None, None, page_table.shape[1], prefix_len, None)
+    n = load_library().meteora_prefix_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), H)
+    if n == 0:
+        raise MeteoraError(-1, "meteora_prefix_attention_workspace_bytes")
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+    ws[:4096].zero_()
+    return ws
+
+
+def meteora_prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix_pages=None, prefix_len: int = 0, cu_tokens=None,
+                             scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None, out=None,
+                             return_lse: bool = False):
+    """Attention of the new tokens' queries [T, heads, dim] over the prefix that all sequences share (prefix_len tokens in
+    prefix_pages) and each one's own pages up to its own token; the batch is that of meteora_cache_append, called after
+    it with the same lengths.  scale defaults to dim^-1/2.  Returns out, or (out, lse[T, heads])."""
+    return (_native or _load_native()).prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix_pages, prefix_len,
+                                                        cu_tokens, scale, workspace, out, return_lse)
 
 
 def meteora_workspace_routing(shape: MeteoraShape, workspace: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -9,9 +9,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+#include <cstring>
 #include <stdexcept>
 #include <string>
 #include <vector>
@@ -382,6 +385,287 @@ PyObject* linear_forward_group(PyObject* const* a) {
     return tuple(out, routing);
 }
 
+// ---- operators on heads -------------------------------------------------------------------------------------------
+// Their calls run on the device of their first tensor, on that device's current stream, whichever device is current.
+
+void* stream_of(const at::Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
+
+const at::Tensor& cuda_tensor(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (!t.is_cuda()) fail(PyExc_ValueError, std::string(name) + " must be a CUDA tensor");
+    return t;
+}
+
+void same_device(const at::Tensor& t, const at::Tensor& first, const char* name) {
+    if (!t.is_cuda() || t.get_device() != first.get_device()) fail(PyExc_ValueError, std::string(name) + " must be on the device of the first tensor");
+}
+
+// x[T, heads, head_dim] with the entries of a head contiguous; any strides of tokens and heads.
+meteora_heads_t heads(const at::Tensor& t, int64_t T, int64_t H, int64_t D, at::ScalarType dt, const at::Tensor& first, const char* name) {
+    same_device(t, first, name);
+    if (t.dim() != 3 || t.size(0) != T || t.size(1) != H || t.size(2) != D || t.scalar_type() != dt)
+        fail(PyExc_ValueError, std::string(name) + ": expected " + size_text({T, H, D}) + " " + c10::toString(dt) + ", got " + size_text(t.sizes()) + " " +
+                                   c10::toString(t.scalar_type()));
+    if (D > 1 && t.stride(2) != 1) fail(PyExc_ValueError, std::string(name) + ": the entries of a head must be contiguous");
+    return meteora_heads_t{t.data_ptr(), t.stride(0), t.stride(1), (int)H};
+}
+
+// Sizes that the library takes as int.
+int small(int64_t v, const char* name) {
+    if (v < 0 || v > INT32_MAX) fail(PyExc_ValueError, std::string(name) + " is out of range");
+    return (int)v;
+}
+
+// The rotary embedding (binding.MeteoraRotary, a buffer of the struct's bytes), or nullptr for None.
+struct Rotary {
+    meteora_rotary_t value;
+    const meteora_rotary_t* ptr = nullptr;
+    explicit Rotary(PyObject* o) {
+        if (o == Py_None) return;
+        Py_buffer b;
+        if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw PySet{};
+        const bool fits = b.len == (Py_ssize_t)sizeof(value);
+        if (fits) memcpy(&value, b.buf, sizeof(value));
+        PyBuffer_Release(&b);
+        if (!fits) fail(PyExc_TypeError, "rot must come from meteora_rotary_init");
+        ptr = &value;
+    }
+};
+
+struct Positions {
+    const void* ptr = nullptr;
+    int wide = 0;
+    Positions(PyObject* o, int64_t T, const at::Tensor& first, bool needed) {
+        if (o == Py_None && !needed) return;
+        const at::Tensor& t = tensor(o, "positions");
+        same_device(t, first, "positions");
+        wide = t.scalar_type() == at::kLong;
+        ptr = dev(t, {T}, wide ? at::kLong : at::kInt, "positions");
+    }
+};
+
+// q (and k, unless None) with results of their shapes.
+struct QkPair {
+    const at::Tensor& q;
+    int64_t T, D;
+    at::ScalarType dt;
+    meteora_dtype_t code;
+    bool has_k;
+    at::Tensor out[2];
+    meteora_heads_t in[2], to[2];
+    QkPair(PyObject* qo, PyObject* ko, PyObject* out_q, PyObject* out_k) : q(cuda_tensor(qo, "q")) {
+        dims(q, 3, "q");
+        T = q.size(0), D = q.size(2), dt = q.scalar_type(), code = dtype_code(q), has_k = ko != Py_None;
+        small(T, "T");
+        in[0] = heads(q, T, q.size(1), D, dt, q, "q");
+        if (has_k) {
+            const at::Tensor& k = tensor(ko, "k");
+            dims(k, 3, "k");
+            in[1] = heads(k, T, k.size(1), D, dt, q, "k");
+        } else if (out_k != Py_None) {
+            fail(PyExc_ValueError, "out_k without k");
+        }
+        PyObject* const given[2] = {out_q, out_k};
+        for (int i = 0; i < (has_k ? 2 : 1); ++i) {
+            out[i] = given[i] != Py_None ? tensor(given[i], i ? "out_k" : "out_q") : empty({T, in[i].heads, D}, dt, q);
+            to[i] = heads(out[i], T, in[i].heads, D, dt, q, i ? "out_k" : "out_q");
+        }
+    }
+    PyObject* result(int i) const { return i && !has_k ? keep(Py_None) : wrap(out[i]); }
+};
+
+const void* gain_of(PyObject* o, int64_t D, at::ScalarType dt, const at::Tensor& first, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    same_device(t, first, name);
+    return dev(t, {D}, dt, name);
+}
+
+// (q, k or None, positions, rot, inverse, out_q or None, out_k or None) -> (q', k' or None)
+PyObject* rotary(PyObject* const* a) {
+    const at::Tensor& first = cuda_tensor(a[0], "q");
+    const c10::cuda::CUDAGuard guard(first.device());
+    QkPair p(a[0], a[1], a[5], a[6]);
+    const Positions pos(a[2], p.T, first, true);
+    const Rotary rot(a[3]);
+    const int inverse = PyObject_IsTrue(a[4]) == 1;
+    void* const st = stream_of(first);
+    check(released([&] {
+              return meteora_rotary(&p.in[0], p.has_k ? &p.in[1] : nullptr, &p.to[0], p.has_k ? &p.to[1] : nullptr, pos.ptr, pos.wide, (int)p.T,
+                                    (int)p.D, p.code, rot.ptr, inverse, st);
+          }),
+          "meteora_rotary");
+    return tuple(p.result(0), p.result(1));
+}
+
+// (q, k or None, q_gain, k_gain, positions, rot or None, eps, out_q, out_k) -> (q', k' or None)
+PyObject* head_norm_rotary(PyObject* const* a) {
+    const at::Tensor& first = cuda_tensor(a[0], "q");
+    const c10::cuda::CUDAGuard guard(first.device());
+    QkPair p(a[0], a[1], a[7], a[8]);
+    const Rotary rot(a[5]);
+    const Positions pos(a[4], p.T, first, rot.ptr != nullptr);
+    const void* gq = gain_of(a[2], p.D, p.dt, first, "q_gain");
+    const void* gk = p.has_k ? gain_of(a[3], p.D, p.dt, first, "k_gain") : nullptr;
+    const float eps = (float)real(a[6]);
+    void* const st = stream_of(first);
+    check(released([&] {
+              return meteora_head_norm_rotary(&p.in[0], p.has_k ? &p.in[1] : nullptr, gq, gk, &p.to[0], p.has_k ? &p.to[1] : nullptr, pos.ptr,
+                                              pos.wide, (int)p.T, (int)p.D, p.code, rot.ptr, eps, st);
+          }),
+          "meteora_head_norm_rotary");
+    return tuple(p.result(0), p.result(1));
+}
+
+// (dq', dk' or None, q, k or None, q_gain, k_gain, positions, rot or None, eps, workspace) -> (dq, dk, dq_gain, dk_gain)
+PyObject* head_norm_rotary_backward(PyObject* const* a) {
+    const at::Tensor& first = cuda_tensor(a[2], "q");
+    const c10::cuda::CUDAGuard guard(first.device());
+    QkPair p(a[2], a[3], Py_None, Py_None);
+    meteora_heads_t dy[2];
+    dy[0] = heads(tensor(a[0], "dq"), p.T, p.in[0].heads, p.D, p.dt, first, "dq");
+    if (p.has_k) dy[1] = heads(tensor(a[1], "dk"), p.T, p.in[1].heads, p.D, p.dt, first, "dk");
+    const Rotary rot(a[7]);
+    const Positions pos(a[6], p.T, first, rot.ptr != nullptr);
+    const void* gq = gain_of(a[4], p.D, p.dt, first, "q_gain");
+    const void* gk = p.has_k ? gain_of(a[5], p.D, p.dt, first, "k_gain") : nullptr;
+    const float eps = (float)real(a[8]);
+    const size_t need = meteora_head_norm_rotary_backward_workspace_bytes((int)p.T, p.in[0].heads, p.has_k ? p.in[1].heads : 0, (int)p.D);
+    if (need == 0) check(METEORA_ERR_UNSUPPORTED_SHAPE, "meteora_head_norm_rotary_backward");
+    at::Tensor ws = a[9] == Py_None ? empty({(int64_t)need}, at::kByte, first) : tensor(a[9], "workspace");
+    same_device(ws, first, "workspace");
+    if (!ws.is_contiguous()) fail(PyExc_ValueError, "workspace must be contiguous");
+    at::Tensor dgq = empty({p.D}, at::kFloat, first), dgk;
+    if (p.has_k) dgk = empty({p.D}, at::kFloat, first);
+    float *const pq = (float*)dgq.data_ptr(), *const pk = p.has_k ? (float*)dgk.data_ptr() : nullptr;
+    void *const pws = ws.data_ptr(), *const st = stream_of(first);
+    const size_t bytes = ws.nbytes();
+    check(released([&] {
+              return meteora_head_norm_rotary_backward(&dy[0], p.has_k ? &dy[1] : nullptr, &p.in[0], p.has_k ? &p.in[1] : nullptr, gq, gk, &p.to[0],
+                                                       p.has_k ? &p.to[1] : nullptr, pq, pk, pos.ptr, pos.wide, (int)p.T, (int)p.D, p.code, rot.ptr,
+                                                       eps, pws, bytes, st);
+          }),
+          "meteora_head_norm_rotary_backward");
+    return tuple(p.result(0), p.result(1), wrap(dgq), p.has_k ? wrap(dgk) : keep(Py_None));
+}
+
+// k_cache, v_cache [pages, kv_heads, page_size, head_dim], page_table [B, width], lengths [B], cu_tokens [B + 1] or None
+struct PagedBatch {
+    meteora_cache_t cache;
+    meteora_batch_t batch;
+    at::ScalarType dt;
+    int64_t D;
+    PagedBatch(PyObject* kc, PyObject* vc, PyObject* table, PyObject* lengths, PyObject* cu, int64_t T, int64_t prefix_len, const at::Tensor& first) {
+        const at::Tensor &k = tensor(kc, "k_cache"), &v = tensor(vc, "v_cache"), &pt = tensor(table, "page_table"), &len = tensor(lengths, "lengths");
+        dims(k, 4, "k_cache");
+        dims(pt, 2, "page_table");
+        dt = k.scalar_type();
+        D = k.size(3);
+        const int64_t B = pt.size(0);
+        same_device(k, first, "k_cache");
+        same_device(v, first, "v_cache");
+        same_device(pt, first, "page_table");
+        same_device(len, first, "lengths");
+        cache.k = dev(k, k.sizes(), dt, "k_cache");
+        cache.v = dev(v, k.sizes(), dt, "v_cache");
+        cache.n_pages = k.size(0);
+        cache.kv_heads = small(k.size(1), "k_cache");
+        cache.page_size = small(k.size(2), "k_cache");
+        cache.head_dim = small(D, "k_cache");
+        cache.dtype = dtype_code(k);
+        batch.T = small(T, "T");
+        batch.B = small(B, "page_table");
+        batch.table_width = small(pt.size(1), "page_table");
+        batch.page_table = (const int32_t*)dev(pt, {B, pt.size(1)}, at::kInt, "page_table");
+        batch.lengths = (const int32_t*)dev(len, {B}, at::kInt, "lengths");
+        batch.cu_tokens = nullptr;
+        if (cu != Py_None) {
+            same_device(tensor(cu, "cu_tokens"), first, "cu_tokens");
+            batch.cu_tokens = (const int32_t*)dev(cu, {B + 1}, at::kInt, "cu_tokens");
+        }
+        batch.prefix_len = small(prefix_len, "prefix_len");
+        batch.prefix_pages = nullptr;
+    }
+    void prefix(PyObject* pages, const at::Tensor& first) {
+        const int64_t need = cache.page_size > 0 ? ((int64_t)batch.prefix_len + cache.page_size - 1) / cache.page_size : 0;
+        if (pages == Py_None) {
+            if (need > 0) fail(PyExc_ValueError, "prefix_len without prefix_pages");
+            return;
+        }
+        const at::Tensor& t = tensor(pages, "prefix_pages");
+        same_device(t, first, "prefix_pages");
+        dims(t, 1, "prefix_pages");
+        if (t.size(0) < need) fail(PyExc_ValueError, "prefix_pages holds fewer pages than prefix_len takes");
+        batch.prefix_pages = (const int32_t*)dev(t, t.sizes(), at::kInt, "prefix_pages");
+    }
+};
+
+// (k, v, k_cache, v_cache, page_table, lengths, rot or None, cu_tokens or None, prefix_len, q or None, q_gain, k_gain, eps, out_q) -> q' or None
+PyObject* cache_append(PyObject* const* a) {
+    const at::Tensor &k = cuda_tensor(a[0], "k"), &v = tensor(a[1], "v");
+    const c10::cuda::CUDAGuard guard(k.device());
+    dims(k, 3, "k");
+    const int64_t T = k.size(0);
+    PagedBatch p(a[2], a[3], a[4], a[5], a[7], T, integer(a[8]), k);
+    const Rotary rot(a[6]);
+    const meteora_heads_t hk = heads(k, T, p.cache.kv_heads, p.D, p.dt, k, "k"), hv = heads(v, T, p.cache.kv_heads, p.D, p.dt, k, "v");
+    meteora_heads_t hq, ho;
+    at::Tensor out;
+    const bool has_q = a[9] != Py_None;
+    if (has_q) {
+        const at::Tensor& q = tensor(a[9], "q");
+        dims(q, 3, "q");
+        hq = heads(q, T, q.size(1), p.D, p.dt, k, "q");
+        out = a[13] != Py_None ? tensor(a[13], "out_q") : empty({T, q.size(1), p.D}, p.dt, k);
+        ho = heads(out, T, q.size(1), p.D, p.dt, k, "out_q");
+    } else if (a[13] != Py_None || a[10] != Py_None) {
+        fail(PyExc_ValueError, "out_q and q_gain need q");
+    }
+    const void* gq = a[10] != Py_None ? gain_of(a[10], p.D, p.dt, k, "q_gain") : nullptr;
+    const void* gk = a[11] != Py_None ? gain_of(a[11], p.D, p.dt, k, "k_gain") : nullptr;
+    const float eps = (float)real(a[12]);
+    void* const st = stream_of(k);
+    check(released([&] {
+              return meteora_cache_append(&hk, &hv, has_q ? &hq : nullptr, has_q ? &ho : nullptr, gq, gk, eps, rot.ptr, &p.cache, &p.batch, st);
+          }),
+          "meteora_cache_append");
+    return has_q ? wrap(out) : keep(Py_None);
+}
+
+at::Tensor attention_workspace(const PagedBatch& p, int q_heads, const at::Tensor& first) {
+    const size_t need = meteora_prefix_attention_workspace_bytes(&p.cache, &p.batch, q_heads);
+    if (need == 0) check(METEORA_ERR_INVALID_ARG, "meteora_prefix_attention_workspace_bytes");
+    at::Tensor ws = empty({(int64_t)need}, at::kByte, first);
+    void* const st = stream_of(first);
+    check(released([&] { return meteora_workspace_init(ws.data_ptr(), st); }), "meteora_workspace_init");
+    return ws;
+}
+
+// (q, k_cache, v_cache, page_table, lengths, prefix_pages or None, prefix_len, cu_tokens or None, scale or None, workspace, out, return_lse)
+PyObject* prefix_attention(PyObject* const* a) {
+    const at::Tensor& q = cuda_tensor(a[0], "q");
+    const c10::cuda::CUDAGuard guard(q.device());
+    dims(q, 3, "q");
+    const int64_t T = q.size(0), H = q.size(1);
+    PagedBatch p(a[1], a[2], a[3], a[4], a[7], T, integer(a[6]), q);
+    p.prefix(a[5], q);
+    const meteora_heads_t hq = heads(q, T, H, p.D, p.dt, q, "q");
+    at::Tensor made_ws, out = a[10] != Py_None ? tensor(a[10], "out") : empty({T, H, p.D}, p.dt, q), lse;
+    const meteora_heads_t ho = heads(out, T, H, p.D, p.dt, q, "out");
+    if (a[9] == Py_None) made_ws = attention_workspace(p, small(H, "q"), q);
+    const at::Tensor& ws = made_ws.defined() ? made_ws : tensor(a[9], "workspace");
+    same_device(ws, q, "workspace");
+    if (!ws.is_contiguous()) fail(PyExc_ValueError, "workspace must be contiguous");
+    const bool want_lse = PyObject_IsTrue(a[11]) == 1;
+    if (want_lse) lse = empty({T, H}, at::kFloat, q);
+    float* const pl = want_lse ? (float*)lse.data_ptr() : nullptr;
+    const float scale = a[8] == Py_None ? (float)(1.0 / std::sqrt((double)p.D)) : (float)real(a[8]);
+    void *const pws = ws.data_ptr(), *const st = stream_of(q);
+    const size_t bytes = ws.nbytes();
+    check(released([&] { return meteora_prefix_attention(&hq, &p.cache, &p.batch, scale, &ho, pl, pws, bytes, st); }), "meteora_prefix_attention");
+    PyObject* out_obj = a[10] != Py_None ? keep(a[10]) : wrap(out);
+    return want_lse ? tuple(out_obj, wrap(lse)) : out_obj;
+}
+
 PyObject* init(PyObject* const* a) {
     Py_XDECREF(g_error);
     g_error = keep(a[0]);
@@ -393,6 +677,9 @@ PyMethodDef methods[] = {METEORA_METHOD(gate_topk, 5),           METEORA_METHOD(
                          METEORA_METHOD(lora_delta, 9),          METEORA_METHOD(linear_forward, 10),
                          METEORA_METHOD(linear_forward_host, 9), METEORA_METHOD(gate_backward, 9),
                          METEORA_METHOD(linear_forward_group, 9), METEORA_METHOD(init, 1),
+                         METEORA_METHOD(rotary, 7),               METEORA_METHOD(head_norm_rotary, 9),
+                         METEORA_METHOD(head_norm_rotary_backward, 10), METEORA_METHOD(cache_append, 14),
+                         METEORA_METHOD(prefix_attention, 12),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
