@@ -16,7 +16,7 @@ NATIVE_SOURCE = "native.cpp"
 SOURCES = ["api.cu", "host_copy.cu", "gate_topk.cu", "route.cu", "lora.cu", "gemm_simt.cu", "wgemm_tcgen05.cu", "lora_static.cu",
            "gate_backward.cu", "api_heads.cu", "heads.cu", "attend.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0"]
 
 
 def _nvcc() -> str:

@@ -47,7 +47,7 @@ static int check_attend_sizes(const meteora_cache_t* c, const meteora_batch_t* b
     if (c->head_dim > METEORA_MAX_HEAD_DIM || q_heads > 65535 || b->B > METEORA_MAX_BATCH || c->page_size > (1 << 24))
         return METEORA_ERR_UNSUPPORTED_SHAPE;
     if ((long long)b->table_width * c->page_size >= (1LL << 29) || b->prefix_len >= (1 << 29)) return METEORA_ERR_UNSUPPORTED_SHAPE;
-    *z = AttendSizes{b->T, b->B, q_heads, c->kv_heads, c->head_dim, c->page_size, b->table_width, b->prefix_len, c->dtype};
+    *z = AttendSizes{b->T, b->B, q_heads, c->kv_heads, c->head_dim, c->page_size, b->table_width, b->prefix_len, c->n_pages, c->dtype};
     return METEORA_OK;
 }
 

@@ -1,6 +1,5 @@
 // Attention for a batch whose sequences share a prefix, over a paged cache: the plan of a call and its launches.
 #include <algorithm>
-#include <atomic>
 
 #include "attend_mma.cuh"
 #include "attend_simt.cuh"
@@ -25,9 +24,15 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
     const int all = (int)min((long long)s.held + s.tokens, table_keys(p.batch));
     const int seen = (int)min((long long)s.held + (t - s.first) + 1, (long long)all);
     const int piece = own_piece(all, p.own_slots, p.own_min);
-    const int slots = p.prefix_slots + (seen + piece - 1) / piece;
+    int early = p.prefix_slots;                                      // pieces of the prefix, then those of the own tokens
+    if (p.tc.ctas > 0) {
+        const int kv = h / p.group, tiles = p.tc.units / p.kv_heads;
+        const long long x = ((long long)kv * tiles + ((long long)t * p.group + h - kv * p.group) / kPrefixRows) * p.tc.tiles;
+        early = share_of(p.tc, x + p.tc.tiles - 1) - share_of(p.tc, x) + 1;
+    }
+    const int slots = early + (seen + piece - 1) / piece, skip = p.prefix_slots - early;
     float M = -INFINITY;
-    for (int i = lane; i < slots; i += 32) M = fmaxf(M, p.part_ml[i * all_rows + row].x);
+    for (int i = lane; i < slots; i += 32) M = fmaxf(M, p.part_ml[(i + (i < early ? 0 : skip)) * all_rows + row].x);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
     const float base = M == -INFINITY ? 0.f : M;
@@ -36,7 +41,7 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
     float4 acc[2] = {};
     for (int i0 = 0; i0 < slots; i0 += 32) {
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (i0 + lane < slots) ml = p.part_ml[(i0 + lane) * all_rows + row];
+        if (i0 + lane < slots) ml = p.part_ml[(i0 + lane + (i0 + lane < early ? 0 : skip)) * all_rows + row];
         const float w = piece_factor(ml, base);
         const int n = min(32, slots - i0);
 #pragma unroll 4
@@ -44,7 +49,7 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
             const float f = __shfl_sync(0xFFFFFFFFu, w, i), fl = __shfl_sync(0xFFFFFFFFu, ml.y, i);
             if (f == 0.f) continue;              // (a piece in which the row sees nothing; NaN goes on)
             L = fmaf(f, fl, L);
-            const float* o = p.part_o + ((i0 + i) * all_rows + row) * p.dim;
+            const float* o = p.part_o + ((i0 + i + (i0 + i < early ? 0 : skip)) * all_rows + row) * p.dim;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int e = (lane + 32 * c) * 4;
@@ -90,7 +95,6 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
 // ---------------------------------------------------------------------------------------------
 // Plan
 // ---------------------------------------------------------------------------------------------
-constexpr int kMaxSmem = 227 * 1024;
 constexpr int kTargetCtas = 296;         // two CTAs per SM
 constexpr int kMaxOwnItems = 8192;       // a piece that its sequence does not reach is a CTA that leaves at once
 
@@ -129,7 +133,17 @@ static AttendPlan plan_attend(const AttendSizes& z) {
     set_tile(p, 0, plan.wide[0] ? 64 : 16, z.T);
     set_tile(p, 1, plan.wide[1] ? 64 : 16, mean);
     const auto round_up = [](long long v) { return (v + kAttendTile - 1) / kAttendTile * kAttendTile; };
-    if (z.prefix_len > 0) {
+    if (prefix_tc_supported(z)) {
+        // even shares of whole tiles: no more CTAs than SMs, and pieces of two tiles at least where there are as many
+        const long long tiles_of_rows = ((long long)z.T * p.group + kPrefixRows - 1) / kPrefixRows;
+        p.tc.units = (int)(tiles_of_rows * p.kv_heads);
+        p.tc.tiles = (z.prefix_len + 127) / 128;
+        p.tc.ctas = (int)std::max(1LL, std::min(148LL, (long long)p.tc.units * p.tc.tiles));
+        for (int u = 0; u < p.tc.units; ++u) {
+            const long long x = (long long)u * p.tc.tiles;
+            p.prefix_slots = std::max(p.prefix_slots, share_of(p.tc, x + p.tc.tiles - 1) - share_of(p.tc, x) + 1);
+        }
+    } else if (z.prefix_len > 0) {
         const long long units = (long long)p.kv_heads * p.t_tiles[0] * p.g_tiles[0];
         const long long want = std::max(1LL, std::min({(kTargetCtas + units - 1) / units, round_up(z.prefix_len) / kAttendTile, 64LL}));
         p.prefix_piece = (int)round_up((z.prefix_len + want - 1) / want);
@@ -148,37 +162,10 @@ size_t attend_workspace_bytes(const AttendSizes& z) {
     return kHeaderBytes + align_up(rows * z.head_dim * 4, 256) + align_up(rows * 8, 256);
 }
 
-template <auto kernel>
-static int launch_attend(long long ctas, int threads, size_t smem, const AttendParams& p, cudaStream_t st) {
-    if (ctas <= 0) return METEORA_OK;
-    if (smem > 48 * 1024) {
-        static std::atomic<size_t> allowed[64];                     // per device: dynamic shared memory the kernel may have
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
-        if (e == cudaSuccess && (dev >= 64 || allowed[dev].load(std::memory_order_relaxed) < smem)) {
-            // (always the device's largest: a smaller size set by another thread meanwhile would refuse this launch)
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-            if (e == cudaSuccess && dev < 64) allowed[dev].store(kMaxSmem, std::memory_order_relaxed);
-        }
-        if (e != cudaSuccess) return cuda_status(e);
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = tuning().pdl ? 1 : 0;
-    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
-}
-
 template <int DP>
 static int launch_mma(bool wide, const AttendParams& p, cudaStream_t st) {
-    if (wide) return launch_attend<k_attend_mma<DP, 4>>(p.items, 128, AttendMmaShape<DP, 4>::kBytes, p, st);
-    return launch_attend<k_attend_mma<DP, 1>>(p.items, 128, AttendMmaShape<DP, 1>::kBytes, p, st);
+    if (wide) return launch_dependent<k_attend_mma<DP, 4>>(dim3((unsigned)p.items), 128, AttendMmaShape<DP, 4>::kBytes, st, p);
+    return launch_dependent<k_attend_mma<DP, 1>>(dim3((unsigned)p.items), 128, AttendMmaShape<DP, 1>::kBytes, st, p);
 }
 
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,
@@ -200,18 +187,20 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
     const size_t rows = plan.slots * z.T * z.q_heads;
     p.part_o = (float*)((uint8_t*)workspace + kHeaderBytes);
     p.part_ml = (float2*)((uint8_t*)p.part_o + align_up(rows * z.head_dim * 4, 256));
-    const long long prefix_items = (long long)p.prefix_slots * p.kv_heads * p.t_tiles[0] * p.g_tiles[0];
+    const long long prefix_items = p.tc.ctas > 0 ? 0 : (long long)p.prefix_slots * p.kv_heads * p.t_tiles[0] * p.g_tiles[0];
     const long long own_items = z.table_width > 0 ? (long long)p.own_slots * p.kv_heads * p.t_tiles[1] * p.g_tiles[1] : 0;
     if (prefix_items + own_items >= (1LL << 31)) return METEORA_ERR_UNSUPPORTED_SHAPE;
     int rc = METEORA_OK;
-    auto pieces = [&](long long n_prefix, long long n_own, bool wide) {
+    auto pieces = [&](long long n_prefix, long long n_own, bool wide) -> int {
+        if (n_prefix + n_own == 0) return METEORA_OK;
         AttendParams a = p;
         a.prefix_items = (int)n_prefix;
         a.items = (int)(n_prefix + n_own);
         if (plan.mma) return plan.dp == 64 ? launch_mma<64>(wide, a, st) : plan.dp == 128 ? launch_mma<128>(wide, a, st) : launch_mma<256>(wide, a, st);
-        if (z.dtype == METEORA_BF16) return launch_attend<k_attend_simt<__nv_bfloat16>>(a.items, 128, attend_simt_bytes(p.dim), a, st);
-        return launch_attend<k_attend_simt<float>>(a.items, 128, attend_simt_bytes(p.dim), a, st);
+        if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3((unsigned)a.items), 128, attend_simt_bytes(p.dim), st, a);
+        return launch_dependent<k_attend_simt<float>>(dim3((unsigned)a.items), 128, attend_simt_bytes(p.dim), st, a);
     };
+    if (p.tc.ctas > 0 && (rc = launch_prefix_tc(p, st)) != METEORA_OK) return rc;
     if (plan.wide[0] == plan.wide[1]) {
         rc = pieces(prefix_items, own_items, plan.wide[0]);
     } else {
@@ -220,8 +209,8 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
     }
     if (rc != METEORA_OK) return rc;
     const long long join = ((long long)z.T * z.q_heads + 3) / 4;
-    if (z.dtype == METEORA_BF16) return launch_attend<k_attend_join<__nv_bfloat16>>(join, 128, 0, p, st);
-    return launch_attend<k_attend_join<float>>(join, 128, 0, p, st);
+    if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_join<__nv_bfloat16>>(dim3((unsigned)join), 128, 0, st, p);
+    return launch_dependent<k_attend_join<float>>(dim3((unsigned)join), 128, 0, st, p);
 }
 
 }  // namespace meteora

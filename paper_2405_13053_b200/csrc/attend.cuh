@@ -15,6 +15,18 @@
 
 namespace meteora {
 
+// The tensor-core kernel's tiles of the prefix (attend_prefix.cuh), `tiles` per unit of rows, dealt to `ctas` CTAs in even
+// shares: share c is tiles [share_start(c), share_start(c + 1)) of all units in a row.
+struct PrefixShare {
+    int ctas;                      // 0: the prefix runs elsewhere
+    int units, tiles;
+};
+__host__ __device__ inline long long share_start(const PrefixShare& s, int c) { return (long long)s.units * s.tiles * c / s.ctas; }
+// The share that tile x is in: the largest c with share_start(c) <= x.
+__host__ __device__ inline int share_of(const PrefixShare& s, long long x) {
+    return (int)(((x + 1) * s.ctas - 1) / ((long long)s.units * s.tiles));
+}
+
 struct AttendParams {
     const void* q;
     void* out;
@@ -31,12 +43,14 @@ struct AttendParams {
     // rows of a tile, [0] for the prefix and [1] for own tokens: tokens x heads of one kv head; and the tiles there are
     int tile_tokens[2], tile_heads[2], t_tiles[2], g_tiles[2];
     int prefix_items, items;           // of this launch; items [0, prefix_items) are pieces of the prefix
+    PrefixShare tc;
     float* part_o;                 // [slots][T * q_heads][dim]
     float2* part_ml;               // [slots][T * q_heads] (m, l)
     int32_t* status;
 };
 
 constexpr int kAttendTile = 64;    // keys per tile
+constexpr int kPrefixRows = 256;   // rows of a unit of the tensor-core kernel
 
 __host__ __device__ inline int own_piece(int tokens, int own_slots, int own_min) {
     const int even = ((tokens + own_slots - 1) / own_slots + kAttendTile - 1) / kAttendTile * kAttendTile;

@@ -1,0 +1,410 @@
+// The shared prefix of a bf16 batch on the tensor cores: rows of all sequences against the prefix's keys (attend.cuh has
+// the mathematics and where the pieces go).  Included by wgemm_tcgen05.cu after the device helpers it uses.
+//
+// A unit of work is 256 rows (token, head of one kv head's group) x the prefix, in tiles of 128 keys.  The units' tiles are
+// dealt to the CTAs in even shares, one after the other, so that no SM idles behind an uneven number of units; a share that
+// starts or ends inside a unit leaves its part as a piece (prefix_pieces tells the join how many a row has).
+//
+// The rows are two tiles of 128 with a softmax group of four warps each, one thread per row.  Scores S = Q K^T go to TMEM,
+// the group turns them into weights 2^(s - m), rounded to bf16 and stored over the scores they came from, and the second
+// product O += P V takes P from there (A operand in TMEM) and V as it lies (its entries contiguous: the MN-major form of B).
+// While one group works on its scores the tensor core has the other tile's products: S and PV of a tile are 512 cycles
+// each (128 x 128 x 128), a tile's 16384 exponentials 1024 at 16 per cycle, so at 256 rows tensor core and exponentials
+// are nearly even.  A row's reference m is not its running maximum: it stays until the maximum is 8 above it, which
+// leaves weights below 2^8 and spares nearly all rescaling of O.
+//
+// A page that is not there and the keys behind the prefix's end count as -inf, and their values are zeroed in shared memory:
+// what the cache holds there (an infinity, a NaN) would pass a weight of 0.
+#pragma once
+
+#include "attend.cuh"
+
+namespace meteora {
+
+constexpr int kPfxKeys = 128;                        // keys per tile
+constexpr int kPfxRows = kPrefixRows;                // rows per unit
+constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
+
+template <int D> struct PrefixShape {
+    static constexpr int kTileBytes = kPfxKeys * D * 2;
+    static constexpr int kStages = D == 128 ? 5 : 11;              // of keys or values of one tile
+    static constexpr int kBarOff = (2 + kStages) * kTileBytes;     // barriers, then page masks, TMEM slot
+    static constexpr int kSmem = 1024 + kBarOff + (2 * kStages + 11) * 8 + kPfxMasks * 4 + 16;
+};
+
+struct PrefixTcParams {
+    AttendParams a;
+    int box_rows, box_shift;                         // keys per copy: divides the page and the tile
+    int sign;                                        // of the scale: the queries are multiplied by it, scale_log2 is above 0 (a masked
+                                                     // score, -inf, stays one)
+};
+
+// A_i P^T: A from TMEM, B from shared memory.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+          "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+        "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void add2(unsigned long long& a, unsigned long long b) { asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a) : "l"(b)); }
+__device__ __forceinline__ unsigned long long pair2(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair2(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2_of(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixTcParams pp) {
+    typedef PrefixShape<D> S;
+    constexpr int kHalves = D / 64;
+    const AttendParams& p = pp.a;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* const base_ptr = smem_raw + (base - raw);
+    const uint32_t s_q = base, ring = base + 2 * S::kTileBytes;
+    const uint32_t bar_full = base + S::kBarOff, bar_free = bar_full + S::kStages * 8, bar_s = bar_free + S::kStages * 8, bar_p = bar_s + 16,
+                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_tail = bar_q + 16;
+    volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8 + kPfxMasks * 4);
+    const int warp = warp_id(), lane = threadIdx.x & 31;
+    const PrefixShare sh = p.tc;
+    const long long x_lo = share_start(sh, blockIdx.x), x_hi = share_start(sh, blockIdx.x + 1);
+    const int rows_all = p.batch.T * p.group, pair_tiles = (rows_all + kPfxRows - 1) / kPfxRows;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(bar_full + i * 8, 1);
+            mbar_init(bar_free + i * 8, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_s + i * 8, 1);
+            mbar_init(bar_p + i * 8, 128);
+            mbar_init(bar_o + i * 8, 1);
+            mbar_init(bar_ofree + i * 8, 128);
+            mbar_init(bar_q + i * 8, 128);
+        }
+        mbar_init(bar_tail, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);    // S of both tiles, then O of both
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    bool ok = true;
+    int where = 0;
+
+    if (warp == 0) {
+        // ---- copies: K then V of every tile, page by page
+        int n = 0, tails = 0, done = 0;
+        for (long long x = x_lo; x < x_hi && ok; ++x, ++done) {
+            const int unit = (int)(x / sh.tiles), tile = (int)(x - (long long)unit * sh.tiles), h = unit / pair_tiles;
+            const int key0 = tile * kPfxKeys, boxes = kPfxKeys >> pp.box_shift;
+            const int limit = min(kPfxKeys, p.batch.prefix - key0);            // keys of the tile that there are
+            long long page = -1;
+            int at = 0;
+            if (lane < boxes && lane * pp.box_rows < limit) {
+                const int key = key0 + lane * pp.box_rows, slot = key / p.batch.page;
+                at = key - slot * p.batch.page;
+                page = __ldg(p.batch.prefix_pages + slot);
+                if (page < 0 || page >= p.batch.n_pages) page = -1;
+            }
+            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, page >= 0);
+            const bool whole = limit == kPfxKeys && __popc(mask) == boxes;
+            if (lane == 0) s_mask[done % kPfxMasks] = mask;
+            for (int which = 0; which < 2 && ok; ++which, ++n) {
+                const int st = n % S::kStages, round = n / S::kStages;
+                if (round > 0 && !mbar_wait_warp(bar_free + st * 8, (round & 1) ^ 1)) {
+                    ok = false, where = 1;
+                    break;
+                }
+                const uint32_t dst = ring + st * S::kTileBytes;
+                const bool slow = which == 1 && !whole;                        // values that have to be zeroed
+                const uint32_t bar = slow ? bar_tail : bar_full + st * 8;
+                if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(mask) * pp.box_rows * D * 2);
+                __syncwarp();
+                if (page >= 0) {
+                    const CUtensorMap* tm = which ? &tmV : &tmK;
+#pragma unroll
+                    for (int c = 0; c < kHalves; ++c)
+                        tma_load_3d(dst + c * (kPfxKeys * 128) + lane * pp.box_rows * 128, tm, c * 64, at, (int)page * p.kv_heads + h, bar);
+                }
+                __syncwarp();
+                if (slow) {
+                    if (!mbar_wait_warp(bar_tail, tails & 1)) {
+                        ok = false, where = 2;
+                        break;
+                    }
+                    ++tails;
+                    for (int r = 0; r < kPfxKeys; ++r) {
+                        if (r < limit && (mask >> (r >> pp.box_shift) & 1u)) continue;
+                        if (lane < kHalves * 8)
+                            *reinterpret_cast<uint4*>(base_ptr + (dst - base) + (lane >> 3) * (kPfxKeys * 128) + r * 128 + (lane & 7) * 16) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_full + st * 8);
+                }
+            }
+        }
+        if (!ok)                                                               // copies in flight land before the CTA leaves
+            for (int q = max(0, n - S::kStages); q < n; ++q) mbar_wait_warp(bar_full + (q % S::kStages) * 8, (q / S::kStages) & 1);
+    } else if (warp == 1) {
+        // ---- products
+        const uint32_t idesc_s = instr_desc_bf16(kPfxKeys), idesc_o = instr_desc_bf16(D) | (1u << 16);
+        int n = 0, tiles_of[2] = {0, 0}, segs_of[2] = {0, 0};
+        auto scores = [&](int i, uint32_t k_tile) {
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < D / kUmmaK; ++kk) {
+                    const uint32_t off = (kk >> 2) * (kPfxKeys * 128);
+                    umma_bf16(tmem + i * 128, smem_desc_sw128(s_q + i * S::kTileBytes + off) + (uint64_t)((kk & 3) * 2),
+                              smem_desc_sw128(k_tile + off) + (uint64_t)((kk & 3) * 2), idesc_s, kk != 0);
+                }
+                umma_commit(bar_s + i * 8);
+            }
+            __syncwarp();
+        };
+        auto sums = [&](int i, uint32_t v_tile, bool first) {
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kPfxKeys / kUmmaK; ++kk) {
+                    // 16 keys: two groups of eight rows of 128 bytes, 1024 apart; the next 64 entries a half tile on
+                    const uint64_t db = (smem_desc_sw128(v_tile + kk * 2048) & ~((uint64_t)0x3FFF << 16)) | ((uint64_t)((kPfxKeys * 128) >> 4) << 16);
+                    umma_bf16_ts(tmem + 256 + i * 128, tmem + i * 128 + kk * 8, db, idesc_o, !(first && kk == 0));
+                }
+            }
+            __syncwarp();
+        };
+        auto release = [&](int stage) {
+            if (elect_one()) umma_commit(bar_free + stage * 8);
+            __syncwarp();
+        };
+        auto wait_full = [&](int i) { return mbar_wait_warp(bar_full + (i % S::kStages) * 8, (i / S::kStages) & 1); };
+        for (long long x = x_lo; x < x_hi && ok;) {
+            const int unit = (int)(x / sh.tiles), row0 = unit % pair_tiles * kPfxRows;
+            const int count = (int)(min(x_hi, (long long)(unit + 1) * sh.tiles) - x), active = rows_all - row0 > 128 ? 2 : 1;
+            ok = wait_full(n);
+            for (int i = 0; i < active && ok; ++i) ok = mbar_wait_warp(bar_q + i * 8, segs_of[i] & 1);
+            if (!ok) {
+                where = 3;
+                break;
+            }
+            tc_fence_after();
+            for (int i = 0; i < active; ++i) scores(i, ring + n % S::kStages * S::kTileBytes);
+            release(n % S::kStages);
+            for (int j = 0; j < count && ok; ++j, n += 2) {
+                ok = wait_full(n + 1) && (j + 1 == count || wait_full(n + 2));
+                const uint32_t v_tile = ring + (n + 1) % S::kStages * S::kTileBytes, k_next = ring + (n + 2) % S::kStages * S::kTileBytes;
+                for (int i = 0; i < active && ok; ++i) {
+                    if (j == 0 && segs_of[i] > 0) ok = mbar_wait_warp(bar_ofree + i * 8, (segs_of[i] - 1) & 1);
+                    ok = ok && mbar_wait_warp(bar_p + i * 8, tiles_of[i] & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    ++tiles_of[i];
+                    sums(i, v_tile, j == 0);
+                    if (j + 1 < count) {
+                        scores(i, k_next);
+                    } else {
+                        if (elect_one()) umma_commit(bar_o + i * 8);
+                        __syncwarp();
+                    }
+                }
+                if (!ok) {
+                    where = 4;
+                    break;
+                }
+                release((n + 1) % S::kStages);
+                if (j + 1 < count) release((n + 2) % S::kStages);
+            }
+            for (int i = 0; i < active; ++i) ++segs_of[i];
+            x += count;
+        }
+    } else {
+        // ---- softmax: warps 2 - 5 have the first 128 rows, 6 - 9 the second; a warp's TMEM lanes are those of its number mod 4
+        const int i = warp >= 6, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + 256 + i * 128;
+        int tiles = 0, segs = 0, done = 0;
+        for (long long x = x_lo; x < x_hi && ok;) {
+            const int unit = (int)(x / sh.tiles), h = unit / pair_tiles, row0 = unit % pair_tiles * kPfxRows;
+            const int count = (int)(min(x_hi, (long long)(unit + 1) * sh.tiles) - x), first_tile = (int)(x - (long long)unit * sh.tiles);
+            if (i == 1 && rows_all - row0 <= 128) {                            // no rows for the second tile
+                x += count;
+                done += count;
+                continue;
+            }
+            // queries: each thread its own row
+            const int row = row0 + i * 128 + r;
+            const bool live = row < rows_all;
+            const int t = live ? row / p.group : 0, g = live ? row - t * p.group : 0;
+            {
+                const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(h * p.group + g) * p.q_h;
+                const bool wide = ((uintptr_t)src & 15) == 0;
+                const uint32_t flip = pp.sign < 0 ? 0x80008000u : 0u, keep = pp.sign ? 0xFFFFFFFFu : 0u;
+                uint8_t* const dst = base_ptr + i * S::kTileBytes + r * 128;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (live) {
+                        if (wide) {
+                            v = *reinterpret_cast<const uint4*>(src + c * 8);
+                        } else {
+                            __nv_bfloat16 e[8];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) e[q] = src[c * 8 + q];
+                            memcpy(&v, e, 16);
+                        }
+                    }
+                    v.x = (v.x ^ flip) & keep, v.y = (v.y ^ flip) & keep, v.z = (v.z ^ flip) & keep, v.w = (v.w ^ flip) & keep;
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * (kPfxKeys * 128) + (((c & 7) ^ (r & 7)) << 4)) = v;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(bar_q + i * 8);
+            }
+            float ref = -INFINITY, l = 0.f;
+            for (int j = 0; j < count; ++j, ++tiles, ++done) {
+                ok = mbar_wait(bar_s + i * 8, tiles & 1);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    ok = false, where = 5;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t mask = s_mask[done % kPfxMasks];
+                const int limit = min(kPfxKeys, p.batch.prefix - (first_tile + j) * kPfxKeys);
+                float s[kPfxKeys];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, s + c * 32);
+                tmem_wait_ld();
+                if (limit < kPfxKeys || __popc(mask) < (kPfxKeys >> pp.box_shift)) {
+#pragma unroll
+                    for (int k = 0; k < kPfxKeys; ++k)
+                        if (k >= limit || !(mask >> (k >> pp.box_shift) & 1u)) s[k] = -INFINITY;
+                }
+                float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int k = 4; k < kPfxKeys; k += 4)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) top[q] = fmaxf(top[q], s[k + q]);
+                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+                const bool grow = high > ref + 8.f || (ref == -INFINITY && high > -INFINITY);
+                if (j > 0 && __any_sync(0xFFFFFFFFu, grow)) {
+                    const float f = grow ? exp2_fast(ref - high) : 1.f;
+                    l *= f;
+#pragma unroll
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        tmem_ld32(t_o + c, o);
+                        tmem_wait_ld();
+                        uint32_t w[16];
+#pragma unroll
+                        for (int hh = 0; hh < 2; ++hh) {
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) w[q] = __float_as_uint(o[hh * 16 + q] * f);
+                            tmem_st16(t_o + c + hh * 16, w);
+                        }
+                    }
+                }
+                if (grow) ref = high;
+                const float m = ref == -INFINITY ? 0.f : ref;
+                const unsigned long long sc2 = pair2(p.scale_log2, p.scale_log2), m2 = pair2(-m, -m);
+                unsigned long long sum2[2] = {0ull, 0ull};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        float a, b;
+                        unpair2(fma2_of(pair2(s[c * 32 + 2 * q], s[c * 32 + 2 * q + 1]), sc2, m2), a, b);
+                        a = exp2_fast(a);
+                        b = exp2_fast(b);
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(b), "f"(a));
+                        add2(sum2[q & 1], bf16x2_to_f32x2(w[q]));
+                    }
+                    tmem_st16(t_s + c * 16, w);
+                }
+                add2(sum2[0], sum2[1]);
+                float a, b;
+                unpair2(sum2[0], a, b);
+                l += a + b;
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar_p + i * 8);
+            }
+            if (!ok) break;
+            ok = mbar_wait(bar_o + i * 8, segs & 1);
+            if (!__all_sync(0xFFFFFFFFu, ok)) {
+                ok = false, where = 6;
+                break;
+            }
+            tc_fence_after();
+            const int slot = (int)blockIdx.x - share_of(sh, (long long)unit * sh.tiles);
+            const size_t out = (size_t)slot * p.batch.T * p.q_heads + (size_t)t * p.q_heads + h * p.group + g;
+            if (live) p.part_ml[out] = make_float2(ref, l);
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                tmem_ld32(t_o + c, o);
+                tmem_wait_ld();
+                if (live)
+#pragma unroll
+                    for (int q = 0; q < 32; q += 4)
+                        *reinterpret_cast<float4*>(p.part_o + out * D + c + q) = make_float4(o[q], o[q + 1], o[q + 2], o[q + 3]);
+            }
+            tc_fence_before();
+            mbar_arrive(bar_ofree + i * 8);
+            ++segs;
+            x += count;
+        }
+    }
+    if (!ok && where && lane == 0) {
+        atomicExch(p.status, 1);
+        atomicExch(p.status + 1, 4500 + where);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+}  // namespace meteora

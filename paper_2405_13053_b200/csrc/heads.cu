@@ -317,20 +317,6 @@ __global__ void __launch_bounds__(1024) k_gain_sums(const float* part, int q_cta
 // ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
-template <typename K, typename P>
-static int launch_heads(K kernel, dim3 grid, int threads, const P& p, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = tuning().pdl ? 1 : 0;
-    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, p));
-}
-
 static int pow2_at_least(int v) {
     int l = 1;
     while (l < v) l *= 2;
@@ -398,12 +384,12 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     const int threads = (p.groups * p.lanes + 31) / 32 * 32;
     const dim3 grid(args.T, split);
     if (args.dtype == METEORA_BF16) {
-        if (ve == 8) return launch_heads(k_head_pass<__nv_bfloat16, 8, 1>, grid, threads, p, st);
-        if (ve == 4) return launch_heads(k_head_pass<__nv_bfloat16, 4, 1>, grid, threads, p, st);
-        return launch_heads(k_head_pass<__nv_bfloat16, 1, 4>, grid, threads, p, st);
+        if (ve == 8) return launch_dependent<k_head_pass<__nv_bfloat16, 8, 1>>(grid, threads, 0, st, p);
+        if (ve == 4) return launch_dependent<k_head_pass<__nv_bfloat16, 4, 1>>(grid, threads, 0, st, p);
+        return launch_dependent<k_head_pass<__nv_bfloat16, 1, 4>>(grid, threads, 0, st, p);
     }
-    if (ve == 4) return launch_heads(k_head_pass<float, 4, 1>, grid, threads, p, st);
-    return launch_heads(k_head_pass<float, 1, 4>, grid, threads, p, st);
+    if (ve == 4) return launch_dependent<k_head_pass<float, 4, 1>>(grid, threads, 0, st, p);
+    return launch_dependent<k_head_pass<float, 1, 4>>(grid, threads, 0, st, p);
 }
 
 // CTAs of the gradient kernel: a few per SM, each with at least a tile of tokens; q and k get shares as their heads are.
@@ -452,23 +438,15 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
     const dim3 grid(p.q_ctas + k_ctas);
     int rc = METEORA_OK;
     if (args.dtype == METEORA_BF16)
-        rc = ve == 8   ? launch_heads(k_head_grad<__nv_bfloat16, 8, 1>, grid, kHeadThreads, p, st)
-             : ve == 4 ? launch_heads(k_head_grad<__nv_bfloat16, 4, 1>, grid, kHeadThreads, p, st)
-                       : launch_heads(k_head_grad<__nv_bfloat16, 1, 4>, grid, kHeadThreads, p, st);
+        rc = ve == 8   ? launch_dependent<k_head_grad<__nv_bfloat16, 8, 1>>(grid, kHeadThreads, 0, st, p)
+             : ve == 4 ? launch_dependent<k_head_grad<__nv_bfloat16, 4, 1>>(grid, kHeadThreads, 0, st, p)
+                       : launch_dependent<k_head_grad<__nv_bfloat16, 1, 4>>(grid, kHeadThreads, 0, st, p);
     else
-        rc = ve == 4 ? launch_heads(k_head_grad<float, 4, 1>, grid, kHeadThreads, p, st)
-                     : launch_heads(k_head_grad<float, 1, 4>, grid, kHeadThreads, p, st);
+        rc = ve == 4 ? launch_dependent<k_head_grad<float, 4, 1>>(grid, kHeadThreads, 0, st, p)
+                     : launch_dependent<k_head_grad<float, 1, 4>>(grid, kHeadThreads, 0, st, p);
     if (rc != METEORA_OK) return rc;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((x[1].heads ? 2 : 1) * ((p.dim + 31) / 32));
-    cfg.blockDim = dim3(1024);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = tuning().pdl ? 1 : 0;
-    return cuda_status(cudaLaunchKernelEx(&cfg, k_gain_sums, (const float*)part, p.q_ctas, k_ctas, p.dim, dq_gain, dk_gain));
+    const dim3 sums((x[1].heads ? 2 : 1) * ((p.dim + 31) / 32));
+    return launch_dependent<k_gain_sums>(sums, 1024, 0, st, (const float*)part, p.q_ctas, k_ctas, p.dim, dq_gain, dk_gain);
 }
 
 }  // namespace meteora

@@ -1,9 +1,38 @@
 // Launchers of the operators on heads (heads.cu, attend.cu), called by their C ABI (api_heads.cu) with checked arguments.
 #pragma once
 
-#include "heads.cuh"
+#include <atomic>
+
+#include "attend.cuh"
 
 namespace meteora {
+
+// A launch that may be set up under the kernel ahead (every kernel here waits for it before it touches memory).
+template <auto kernel, typename... A>
+int launch_dependent(dim3 grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
+    if (smem > 48 * 1024) {
+        static std::atomic<bool> allowed[64];                       // per device; always the device's largest, for all sizes at once
+        constexpr int kMaxSmem = 227 * 1024;
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess && (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed))) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+            if (e == cudaSuccess && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+        }
+        if (e != cudaSuccess) return cuda_status(e);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = tuning().pdl ? 1 : 0;
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
 
 struct HeadRows {
     meteora_heads_t in;
@@ -29,8 +58,12 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
 
 struct AttendSizes {
     int T, B, q_heads, kv_heads, head_dim, page_size, table_width, prefix_len;
+    long long n_pages;
     meteora_dtype_t dtype;
 };
+// wgemm_tcgen05.cu: the prefix on the tensor cores
+bool prefix_tc_supported(const AttendSizes& z);
+int launch_prefix_tc(const AttendParams& p, cudaStream_t st);
 size_t attend_workspace_bytes(const AttendSizes& z);
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,
                             const BatchView& batch, const AttendSizes& z, float scale, void* workspace, cudaStream_t st);

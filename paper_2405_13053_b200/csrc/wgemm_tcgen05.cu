@@ -25,6 +25,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "launch_heads.cuh"
 #include "select.cuh"
 
 namespace meteora {
@@ -758,6 +759,7 @@ k_wgemm(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ CUtens
 #include "wgemm_persist.cuh"
 #include "gate_dwg.cuh"
 #include "expand_tile.cuh"
+#include "attend_prefix.cuh"
 
 namespace meteora {
 
@@ -3041,6 +3043,53 @@ int describe_plan(const meteora_shape_t& s, char* buf, size_t n) {
                     "smem=%zu expand=%s",
                     fp.why, routing + 1, tp.S, row_tiles * pl.splits * pl.n_tiles, pl.splits, pl.BN, pl.stages, pl.kc, pl.smem,
                     pl.lora_mma ? "mma" : "simt");
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention over a shared prefix (attend_prefix.cuh)
+// ------------------------------------------------------------------------------------------------
+// Keys per copy: the largest power of two that divides the page and the tile.
+static int prefix_box_rows(int page_size) {
+    int r = 1;
+    while (r < kPfxKeys && page_size % (2 * r) == 0) r *= 2;
+    return r;
+}
+
+bool prefix_tc_supported(const AttendSizes& z) {
+    const long long rows = (long long)z.T * (z.q_heads / z.kv_heads);
+    return z.dtype == METEORA_BF16 && (z.head_dim == 64 || z.head_dim == 128) && prefix_box_rows(z.page_size) >= 8 && z.prefix_len > 0 && rows > 16 &&
+           rows < (1LL << 31) - kPfxRows && z.n_pages > 0 && z.n_pages * z.kv_heads < (1LL << 31);
+}
+
+// Tensor map of a cache [pages * kv_heads][page_size][D]: boxes of 64 entries x `rows` keys, 128-byte swizzled.
+static int get_cache_map(const void* ptr, int D, int page_size, long long planes, int rows, CUtensorMap* out) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return METEORA_ERR_CUDA;
+    const cuuint64_t gdim[3] = {(cuuint64_t)D, (cuuint64_t)page_size, (cuuint64_t)planes};
+    const cuuint64_t gstride[2] = {(cuuint64_t)D * 2, (cuuint64_t)D * 2 * page_size};
+    const cuuint32_t box[3] = {64, (cuuint32_t)rows, 1}, estride[3] = {1, 1, 1};
+    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? METEORA_OK : METEORA_ERR_CUDA;
+}
+
+template <int D>
+static int launch_prefix_tc_d(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixTcParams& pp, cudaStream_t st) {
+    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.tc.ctas), kThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
+}
+
+int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
+    PrefixTcParams pp = {};
+    pp.a = p;
+    pp.box_rows = prefix_box_rows(p.batch.page);
+    while ((1 << pp.box_shift) < pp.box_rows) ++pp.box_shift;
+    pp.sign = p.scale_log2 < 0.f ? -1 : p.scale_log2 > 0.f ? 1 : 0;
+    pp.a.scale_log2 = pp.sign ? fabsf(p.scale_log2) : 1.f;
+    CUtensorMap tk, tv;
+    int rc;
+    if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tk)) != METEORA_OK) return rc;
+    if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tv)) != METEORA_OK) return rc;
+    return p.dim == 64 ? launch_prefix_tc_d<64>(tk, tv, pp, st) : launch_prefix_tc_d<128>(tk, tv, pp, st);
 }
 
 // Knob wait_limit_us: the limit of the bounded device-side waits on the current device (0: the default, about a second).
