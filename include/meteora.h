@@ -493,7 +493,7 @@ int meteora_cache_append(const meteora_heads_t* k, const meteora_heads_t* v, con
  *   lse        optional fp32 [T, q_heads]: logarithm of the row's sum of exp(scale * q . k), -inf for a row that sees none.
  *   workspace  meteora_prefix_attention_workspace_bytes(...) bytes (sizes of cache and batch are read, no pointers), 16-byte
  *              aligned, its header zeroed once (meteora_workspace_init); meteora_workspace_status reads its status word.
- * table_width * page_size and prefix_len stay below 2^29.  Scores, weights' sums and the output are held in fp32; on
+ * table_width * page_size and prefix_len stay below 2^29, T * q_heads below 2^31 - 4096.  Scores, weights' sums and the output are held in fp32; on
  * bf16 caches the weights are rounded to bf16 for the product with the values and enter their sum rounded alike.
  * A value that is no finite number reaches the rows that see its token and no others.
  */

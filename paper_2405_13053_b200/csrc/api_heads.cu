@@ -47,6 +47,7 @@ static int check_attend_sizes(const meteora_cache_t* c, const meteora_batch_t* b
     if (c->head_dim > METEORA_MAX_HEAD_DIM || q_heads > 65535 || b->B > METEORA_MAX_BATCH || c->page_size > (1 << 24))
         return METEORA_ERR_UNSUPPORTED_SHAPE;
     if ((long long)b->table_width * c->page_size >= (1LL << 29) || b->prefix_len >= (1 << 29)) return METEORA_ERR_UNSUPPORTED_SHAPE;
+    if ((long long)b->T * q_heads >= (1LL << 31) - 4096) return METEORA_ERR_UNSUPPORTED_SHAPE;
     *z = AttendSizes{b->T, b->B, q_heads, c->kv_heads, c->head_dim, c->page_size, b->table_width, b->prefix_len, c->n_pages, c->dtype};
     return METEORA_OK;
 }
@@ -246,7 +247,9 @@ int meteora_prefix_attention(const meteora_heads_t* q, const meteora_cache_t* ca
     if (T == 0 || batch->B == 0) return METEORA_OK;
     if (!workspace || (batch->prefix_len > 0 && !batch->prefix_pages)) return METEORA_ERR_INVALID_ARG;
     if ((uintptr_t)workspace % 16 != 0 || (uintptr_t)lse % 4 != 0) return METEORA_ERR_MISALIGNED;
-    if (workspace_bytes < attend_workspace_bytes(z)) return METEORA_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = attend_workspace_bytes(z);
+    if (need == 0) return METEORA_ERR_UNSUPPORTED_SHAPE;
+    if (workspace_bytes < need) return METEORA_ERR_WORKSPACE_TOO_SMALL;
     return launch_prefix_attention(*q, *out, lse, *cache, view_of(*batch, *cache), z, scale, workspace, (cudaStream_t)stream);
 }
 

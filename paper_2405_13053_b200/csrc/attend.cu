@@ -7,170 +7,257 @@
 
 namespace meteora {
 
-// A row's slots joined, one warp per row: the common maximum first, then sums in the order of the slots.
-template <typename E>
-__global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendParams p) {
-    const int lane = threadIdx.x & 31;
-    const size_t all_rows = (size_t)p.batch.T * p.q_heads;
-    const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+// A row's pieces of one launch: the first one's row, and how many there are, `rows` of the space apart.
+struct RowPieces {
+    long long row;
+    int n;
+};
+__device__ __forceinline__ RowPieces row_pieces(const PieceSpace& s, int W, uint32_t x0, int tiles, int unit, int r) {
+    if (tiles <= 0 || W <= 0) return RowPieces{0, 0};
+    const Shares shares((uint32_t)W, share_count(s, (uint32_t)W));
+    const int c0 = (int)shares.of(x0), n = (int)shares.of(x0 + (uint32_t)tiles - 1) - c0 + 1;
+    return RowPieces{(long long)(unit + c0) * s.rows + r, unit + c0 + n <= s.pieces ? n : 0};
+}
+
+// The pieces of one token's heads joined: the common maximum first, then their sum in order.  kWarps == 1: a warp takes
+// `heads_each` heads one after the other (a lane works out each one's pieces beforehand).  kWarps > 1, where the rows are
+// too few to hide one another's latency: a CTA per row, warp w sums pieces w, w + kWarps, ..., then the warps in order.
+template <typename E, int kWarps>
+__global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join(const __grid_constant__ AttendParams p, const int heads_each) {
+    __shared__ float4 s_acc[kWarps == 1 ? 1 : kWarps][64];
+    __shared__ float s_l[kWarps == 1 ? 1 : kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = kWarps == 1 ? 0 : warp;
+    const int t = blockIdx.x, h0 = (kWarps == 1 ? (int)blockIdx.y * 4 + warp : (int)blockIdx.y) * heads_each;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (row >= all_rows) return;
-    const int t = (int)(row / p.q_heads), h = (int)(row - (size_t)t * p.q_heads);
+    if (h0 >= p.q_heads) return;
     const int b = sequence_of(p.batch, t, lane);
     if (b < 0) return;
     const SequenceView s = sequence_view(p.batch, b);
-    if (s.held < 0) return;
-    const int all = (int)min((long long)s.held + s.tokens, table_keys(p.batch));
-    const int seen = (int)min((long long)s.held + (t - s.first) + 1, (long long)all);
-    const int piece = own_piece(all, p.own_slots, p.own_min);
-    int early = p.prefix_slots;                                      // pieces of the prefix, then those of the own tokens
-    if (p.tc.ctas > 0) {
-        const int kv = h / p.group, tiles = p.tc.units / p.kv_heads;
-        const long long x = ((long long)kv * tiles + ((long long)t * p.group + h - kv * p.group) / kPrefixRows) * p.tc.tiles;
-        early = share_of(p.tc, x + p.tc.tiles - 1) - share_of(p.tc, x) + 1;
+    if (s.held < 0 || t >= s.first + s.tokens) return;
+    RowPieces early = {}, late = {};
+    if (lane < heads_each && h0 + lane < p.q_heads) {
+        const int h = h0 + lane, kv = (int)p.by_group.of((unsigned)h), g = h - kv * p.group;
+        if (p.batch.prefix > 0) {
+            const int i = t * p.group + g, rt = (int)((unsigned)i / (unsigned)p.prefix.rows), n_rt = row_tiles(p, p.batch.T, p.prefix.rows);
+            const int tiles = (p.batch.prefix + (1 << p.prefix.shift) - 1) >> p.prefix.shift;
+            const int unit = p.tc ? kv * n_rt + rt : rt * p.kv_heads + kv;
+            const int W = p.prefix.total >= 0 ? p.prefix.total : p.total[0];
+            early = row_pieces(p.prefix, W, (uint32_t)unit * (uint32_t)tiles, tiles, unit, i - rt * p.prefix.rows);
+        }
+        const int seen = min(s.held + (t - s.first) + 1, s.all);
+        if (seen > 0) {
+            const int i = (t - s.first) * p.group + g, rt = (int)((unsigned)i / (unsigned)p.own.rows), in = rt * p.kv_heads + kv;
+            const int up = (1 << p.own.shift) - 1;
+            const uint32_t x0 = (uint32_t)p.first_tile[b] + (uint32_t)in * (uint32_t)((s.all + up) >> p.own.shift);
+            late = row_pieces(p.own, p.total[1], x0, (seen + up) >> p.own.shift, p.first_unit[b] + in, i - rt * p.own.rows);
+        }
     }
-    const int slots = early + (seen + piece - 1) / piece, skip = p.prefix_slots - early;
-    float M = -INFINITY;
-    for (int i = lane; i < slots; i += 32) M = fmaxf(M, p.part_ml[(i + (i < early ? 0 : skip)) * all_rows + row].x);
+    for (int head = 0; head < heads_each && h0 + head < p.q_heads; ++head) {
+        const int h = h0 + head;
+        const int early_n = __shfl_sync(0xFFFFFFFFu, early.n, head), n = early_n + __shfl_sync(0xFFFFFFFFu, late.n, head);
+        const long long early_row = __shfl_sync(0xFFFFFFFFu, early.row, head), late_row = __shfl_sync(0xFFFFFFFFu, late.row, head);
+        auto ml_of = [&](int i) {
+            return i < early_n ? p.prefix.ml[early_row + (long long)i * p.prefix.rows] : p.own.ml[late_row + (long long)(i - early_n) * p.own.rows];
+        };
+        float M = -INFINITY;
+        for (int i = lane; i < n; i += 32) M = fmaxf(M, ml_of(i).x);
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
-    const float base = M == -INFINITY ? 0.f : M;
-    const bool quads = p.dim % 4 == 0;
-    float L = 0.f;
-    float4 acc[2] = {};
-    for (int i0 = 0; i0 < slots; i0 += 32) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (i0 + lane < slots) ml = p.part_ml[(i0 + lane + (i0 + lane < early ? 0 : skip)) * all_rows + row];
-        const float w = piece_factor(ml, base);
-        const int n = min(32, slots - i0);
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float f = __shfl_sync(0xFFFFFFFFu, w, i), fl = __shfl_sync(0xFFFFFFFFu, ml.y, i);
-            if (f == 0.f) continue;              // (a piece in which the row sees nothing; NaN goes on)
-            L = fmaf(f, fl, L);
-            const float* o = p.part_o + ((i0 + i + (i0 + i < early ? 0 : skip)) * all_rows + row) * p.dim;
+        for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
+        const float base = M == -INFINITY ? 0.f : M;
+        const bool quads = p.dim % 4 == 0;
+        float L = 0.f;
+        float4 acc[2] = {};
+        constexpr int kAhead = 4;                    // pieces under way at a time
+        for (int i0 = part; i0 < n; i0 += 32 * kWarps) {
+            const int mine = i0 + lane * kWarps, count = min(32, (n - i0 + kWarps - 1) / kWarps);
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (mine < n) ml = ml_of(mine);
+            const float w = piece_factor(ml, base);
+            for (int j = 0; j < count; j += kAhead) {
+                float4 v[kAhead][2];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int e = (lane + 32 * c) * 4;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (quads) {
-                    if (e < p.dim) v = *reinterpret_cast<const float4*>(o + e);
-                } else {
-                    if (e < p.dim) v.x = o[e];
-                    if (e + 1 < p.dim) v.y = o[e + 1];
-                    if (e + 2 < p.dim) v.z = o[e + 2];
-                    if (e + 3 < p.dim) v.w = o[e + 3];
+                for (int a = 0; a < kAhead; ++a) {
+                    const int i = i0 + (j + a) * kWarps;
+                    const float* o = i < early_n ? p.prefix.o + (early_row + (long long)i * p.prefix.rows) * p.dim
+                                                 : p.own.o + (late_row + (long long)(i - early_n) * p.own.rows) * p.dim;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int e = (lane + 32 * c) * 4;
+                        v[a][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (j + a >= count || e >= p.dim) continue;
+                        if (quads) {
+                            v[a][c] = *reinterpret_cast<const float4*>(o + e);
+                        } else {
+                            v[a][c].x = o[e];
+                            if (e + 1 < p.dim) v[a][c].y = o[e + 1];
+                            if (e + 2 < p.dim) v[a][c].z = o[e + 2];
+                            if (e + 3 < p.dim) v[a][c].w = o[e + 3];
+                        }
+                    }
                 }
-                acc[c].x = fmaf(f, v.x, acc[c].x);
-                acc[c].y = fmaf(f, v.y, acc[c].y);
-                acc[c].z = fmaf(f, v.z, acc[c].z);
-                acc[c].w = fmaf(f, v.w, acc[c].w);
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const float f = __shfl_sync(0xFFFFFFFFu, w, (j + a) & 31), fl = __shfl_sync(0xFFFFFFFFu, ml.y, (j + a) & 31);
+                    if (j + a >= count || f == 0.f) continue;            // (a piece in which the row sees nothing; NaN goes on)
+                    L = fmaf(f, fl, L);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        acc[c].x = fmaf(f, v[a][c].x, acc[c].x);
+                        acc[c].y = fmaf(f, v[a][c].y, acc[c].y);
+                        acc[c].z = fmaf(f, v[a][c].z, acc[c].z);
+                        acc[c].w = fmaf(f, v[a][c].w, acc[c].w);
+                    }
+                }
             }
         }
-    }
-    // a row that sees nothing: zeros, and the logarithm of an empty sum
-    const float inv = M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
-    E* const out = (E*)p.out + t * p.out_t + h * p.out_h;
-    const bool wide = quads && ((uintptr_t)p.out | (uintptr_t)(p.out_t * sizeof(E)) | (uintptr_t)(p.out_h * sizeof(E))) % (4 * sizeof(E)) == 0;
+        if (kWarps > 1) {                            // (one head)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int e = (lane + 32 * c) * 4;
-        const float v[4] = {acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv};
-        if (e >= p.dim) continue;
-        if (wide) {
-            HeadVec<E, 4>::store(out + e, HeadVec<E, 4>::pack(v));
-        } else {
+            for (int c = 0; c < 2; ++c) s_acc[part][lane + 32 * c] = acc[c];
+            if (lane == 0) s_l[part] = L;
+            __syncthreads();
+            if (warp > 0) return;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (e + j < p.dim) {
-                    if constexpr (sizeof(E) == 2) out[e + j] = __float2bfloat16_rn(v[j]);
-                    else out[e + j] = v[j];
+            for (int x = 1; x < kWarps; ++x) {
+                L += s_l[x];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float4 v = s_acc[x][lane + 32 * c];
+                    acc[c].x += v.x, acc[c].y += v.y, acc[c].z += v.z, acc[c].w += v.w;
                 }
+            }
         }
+        // a row that sees nothing: zeros, and the logarithm of an empty sum
+        const float inv = M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
+        E* const out = (E*)p.out + t * p.out_t + h * p.out_h;
+        const bool wide = quads && ((uintptr_t)p.out | (uintptr_t)(p.out_t * sizeof(E)) | (uintptr_t)(p.out_h * sizeof(E))) % (4 * sizeof(E)) == 0;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int e = (lane + 32 * c) * 4;
+            const float v[4] = {acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv};
+            if (e >= p.dim) continue;
+            if (wide) {
+                HeadVec<E, 4>::store(out + e, HeadVec<E, 4>::pack(v));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (e + j < p.dim) {
+                        if constexpr (sizeof(E) == 2) out[e + j] = __float2bfloat16_rn(v[j]);
+                        else out[e + j] = v[j];
+                    }
+            }
+        }
+        if (p.lse && lane == 0) p.lse[(size_t)t * p.q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
     }
-    if (p.lse && lane == 0) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------
 // Plan
 // ---------------------------------------------------------------------------------------------
-constexpr int kTargetCtas = 296;         // two CTAs per SM
-constexpr int kMaxOwnItems = 8192;       // a piece that its sequence does not reach is a CTA that leaves at once
-
 struct AttendPlan {
-    AttendParams p;                      // sizes, tiles, pieces
-    bool mma;
-    int dp;                              // entries of a head as the matrix kernel pads them
-    int wide[2];                         // 64 rows a tile for the prefix / own tokens
-    size_t slots;
+    AttendParams p;                      // sizes, and the workspace's places from a null base
+    bool mma, together;                  // matrix instructions; prefix and own tokens in one launch
+    bool fits;                           // fewer than 2^31 tiles
+    size_t bytes;
 };
 
-static void set_tile(AttendParams& p, int which, int rows, int tokens) {
-    p.tile_heads[which] = std::min(p.group, rows);
-    p.tile_tokens[which] = std::max(1, std::min(rows / p.tile_heads[which], std::max(1, tokens)));
-    p.t_tiles[which] = std::max(1, (int)(((long long)p.batch.T + p.tile_tokens[which] - 1) / p.tile_tokens[which]));   // (T = 0: sizes only)
-    p.g_tiles[which] = (p.group + p.tile_heads[which] - 1) / p.tile_heads[which];
+// The kernel that takes units of `rows` rows: its shared memory per CTA and, with 148 SMs, the workers that run at a time
+// (4 CTAs of an SM at most, by registers).
+static size_t pieces_smem(const AttendSizes& z, bool mma, int rows) {
+    if (!mma) return attend_simt_bytes(z.head_dim);
+    const bool wide = rows == 64;
+    if (z.head_dim <= 64) return wide ? AttendMmaShape<64>::kBytes : AttendWarpShape<64>::kBytes;
+    if (z.head_dim <= 128) return wide ? AttendMmaShape<128>::kBytes : AttendWarpShape<128>::kBytes;
+    return wide ? AttendMmaShape<256>::kBytes : AttendWarpShape<256>::kBytes;
+}
+static void set_kernel(PieceSpace& s, const AttendSizes& z, bool mma) {
+    const int ctas = 148 * std::max(1, std::min(4, (int)(228 * 1024 / (pieces_smem(z, mma, s.rows) + 1024))));
+    const bool warps = mma && s.rows == kWarpRows;
+    s.workers = warps ? 4 * ctas : ctas;
+    s.shift = warps ? 4 : 6;
+    s.least_shift = warps ? 2 : 0;               // (64 keys: a piece of fewer costs the join more than it saves)
+    s.total = -1;
 }
 
-static AttendPlan plan_attend(const AttendSizes& z) {
+static AttendPlan plan_attend(const AttendSizes& z, void* workspace) {
     AttendPlan plan = {};
     AttendParams& p = plan.p;
     p.q_heads = z.q_heads;
     p.kv_heads = z.kv_heads;
     p.group = z.q_heads / z.kv_heads;
     p.dim = z.head_dim;
-    p.batch.B = z.B;
-    p.batch.T = z.T;
-    p.batch.width = z.table_width;
-    p.batch.page = z.page_size;
-    p.batch.prefix = z.prefix_len;
+    p.by_group = fixed_div((uint32_t)p.group);
+    p.by_page = fixed_div((uint32_t)z.page_size);
     plan.mma = z.dtype == METEORA_BF16 && z.head_dim % 8 == 0;
-    plan.dp = z.head_dim <= 64 ? 64 : z.head_dim <= 128 ? 128 : 256;
-    const int mean = std::max(1, z.B > 0 ? z.T / z.B : 1);          // new tokens per sequence
-    plan.wide[0] = plan.mma && (long long)z.T * p.group > 16;
-    plan.wide[1] = plan.mma && (long long)mean * p.group > 16;
-    set_tile(p, 0, plan.wide[0] ? 64 : 16, z.T);
-    set_tile(p, 1, plan.wide[1] ? 64 : 16, mean);
-    const auto round_up = [](long long v) { return (v + kAttendTile - 1) / kAttendTile * kAttendTile; };
-    if (prefix_tc_supported(z)) {
-        // even shares of whole tiles: no more CTAs than SMs, and pieces of two tiles at least where there are as many
-        const long long tiles_of_rows = ((long long)z.T * p.group + kPrefixRows - 1) / kPrefixRows;
-        p.tc.units = (int)(tiles_of_rows * p.kv_heads);
-        p.tc.tiles = (z.prefix_len + 127) / 128;
-        p.tc.ctas = (int)std::max(1LL, std::min(148LL, (long long)p.tc.units * p.tc.tiles));
-        for (int u = 0; u < p.tc.units; ++u) {
-            const long long x = (long long)u * p.tc.tiles;
-            p.prefix_slots = std::max(p.prefix_slots, share_of(p.tc, x + p.tc.tiles - 1) - share_of(p.tc, x) + 1);
-        }
+    p.tc = prefix_tc_supported(z);
+    const long long rows = (long long)z.T * p.group, mean = std::max(1, z.B > 0 ? z.T / z.B : 1);    // mean: new tokens of a sequence
+    // 64 rows at a time where there are more than 16: of the prefix all of them, of own tokens a sequence's mean
+    p.prefix.rows = p.tc ? kPrefixRows : plan.mma && rows > 16 ? 64 : 16;
+    p.own.rows = plan.mma && mean * p.group > 16 ? 64 : 16;
+    plan.together = !p.tc && z.prefix_len > 0 && p.prefix.rows == p.own.rows;
+    const auto units = [&](int r) { return (rows + r - 1) / r * z.kv_heads; };
+    size_t off = kHeaderBytes;
+    const auto take = [&](size_t bytes) {
+        uint8_t* at = workspace ? (uint8_t*)workspace + off : nullptr;
+        off += align_up(bytes, 256);
+        return at;
+    };
+    const auto space = [&](PieceSpace& s, long long n_units) {
+        s.pieces = n_units + s.workers;
+        s.o = (float*)take((size_t)s.pieces * s.rows * z.head_dim * 4);
+        s.ml = (float2*)take((size_t)s.pieces * s.rows * 8);
+    };
+    const long long prefix_units = z.prefix_len > 0 ? units(p.prefix.rows) : 0;
+    set_kernel(p.own, z, plan.mma);
+    space(p.own, units(p.own.rows) + (long long)z.B * z.kv_heads + (plan.together ? prefix_units : 0));
+    if (plan.together) {
+        p.prefix = p.own;
     } else if (z.prefix_len > 0) {
-        const long long units = (long long)p.kv_heads * p.t_tiles[0] * p.g_tiles[0];
-        const long long want = std::max(1LL, std::min({(kTargetCtas + units - 1) / units, round_up(z.prefix_len) / kAttendTile, 64LL}));
-        p.prefix_piece = (int)round_up((z.prefix_len + want - 1) / want);
-        p.prefix_slots = (z.prefix_len + p.prefix_piece - 1) / p.prefix_piece;
+        set_kernel(p.prefix, z, plan.mma);
+        if (p.tc) {
+            p.prefix.shift = 7;
+            p.prefix.least_shift = 0;
+            p.prefix.total = (int)(prefix_units * ((z.prefix_len + kPrefixTile - 1) / kPrefixTile));
+            p.prefix.workers = std::max(1, std::min(148, p.prefix.total));
+        }
+        space(p.prefix, prefix_units);
     }
-    const long long keys = (long long)z.table_width * z.page_size, units = (long long)p.kv_heads * p.t_tiles[1] * p.g_tiles[1];
-    p.own_min = (int)std::min(512LL, std::max((long long)kAttendTile, round_up(keys * units / kTargetCtas)));
-    p.own_slots = (int)std::max(1LL, std::min({(keys + p.own_min - 1) / p.own_min, std::max(8LL, kMaxOwnItems / units), 64LL}));
-    plan.slots = (size_t)p.prefix_slots + (keys > 0 ? p.own_slots : 0);
+    p.total = (int32_t*)take(8);
+    p.first_tile = (int32_t*)take((size_t)z.B * 4);
+    p.first_unit = (int32_t*)take((size_t)z.B * 4);
+    p.status = (int32_t*)workspace;
+    plan.bytes = off;
+    // tiles of a launch at most, by the tables' room
+    const auto most = [&](const PieceSpace& s, long long n_units, long long keys) { return n_units * ((keys >> s.shift) + 1); };
+    const long long own_most = most(p.own, units(p.own.rows) + (long long)z.B * z.kv_heads, (long long)z.table_width * z.page_size);
+    plan.fits = own_most + (z.prefix_len > 0 ? most(p.prefix, prefix_units, z.prefix_len) : 0) < (1LL << 31);
     return plan;
 }
 
 size_t attend_workspace_bytes(const AttendSizes& z) {
-    const AttendPlan plan = plan_attend(z);
-    const size_t rows = plan.slots * z.T * z.q_heads;
-    return kHeaderBytes + align_up(rows * z.head_dim * 4, 256) + align_up(rows * 8, 256);
+    const AttendPlan plan = plan_attend(z, nullptr);
+    return plan.fits ? plan.bytes : 0;
 }
 
 template <int DP>
-static int launch_mma(bool wide, const AttendParams& p, cudaStream_t st) {
-    if (wide) return launch_dependent<k_attend_mma<DP, 4>>(dim3((unsigned)p.items), 128, AttendMmaShape<DP, 4>::kBytes, st, p);
-    return launch_dependent<k_attend_mma<DP, 1>>(dim3((unsigned)p.items), 128, AttendMmaShape<DP, 1>::kBytes, st, p);
+static int launch_mma(const AttendParams& p, cudaStream_t st) {
+    if (p.here.rows == 64) return launch_dependent<k_attend_mma<DP>>(dim3(p.here.workers), 128, AttendMmaShape<DP>::kBytes, st, p);
+    return launch_attend_warp(p, DP, st);
+}
+
+template <typename E>
+static int launch_join(const AttendParams& p, cudaStream_t st) {
+    const long long rows = (long long)p.batch.T * p.q_heads;
+    if (rows <= 1184)                            // 8 CTAs per SM
+        return launch_dependent<k_attend_join<E, 8>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1);
+    const int each = (int)std::max(1LL, std::min(32LL, rows / (148 * 48)));       // heads per warp: as many as leave every SM 48 warps
+    const int warps = (p.q_heads + each - 1) / each;
+    return launch_dependent<k_attend_join<E, 1>>(dim3(p.batch.T, (warps + 3) / 4), 128, 0, st, p, each);
 }
 
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,
                             const BatchView& batch, const AttendSizes& z, float scale, void* workspace, cudaStream_t st) {
-    AttendPlan plan = plan_attend(z);
+    AttendPlan plan = plan_attend(z, workspace);
     AttendParams& p = plan.p;
     p.batch = batch;
     p.q = q.data;
@@ -183,34 +270,20 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
     p.k = cache.k;
     p.v = cache.v;
     p.scale_log2 = scale * 1.4426950408889634f;
-    p.status = (int32_t*)workspace;
-    const size_t rows = plan.slots * z.T * z.q_heads;
-    p.part_o = (float*)((uint8_t*)workspace + kHeaderBytes);
-    p.part_ml = (float2*)((uint8_t*)p.part_o + align_up(rows * z.head_dim * 4, 256));
-    const long long prefix_items = p.tc.ctas > 0 ? 0 : (long long)p.prefix_slots * p.kv_heads * p.t_tiles[0] * p.g_tiles[0];
-    const long long own_items = z.table_width > 0 ? (long long)p.own_slots * p.kv_heads * p.t_tiles[1] * p.g_tiles[1] : 0;
-    if (prefix_items + own_items >= (1LL << 31)) return METEORA_ERR_UNSUPPORTED_SHAPE;
-    int rc = METEORA_OK;
-    auto pieces = [&](long long n_prefix, long long n_own, bool wide) -> int {
-        if (n_prefix + n_own == 0) return METEORA_OK;
+    const auto pieces = [&](bool prefix, bool own) -> int {
         AttendParams a = p;
-        a.prefix_items = (int)n_prefix;
-        a.items = (int)(n_prefix + n_own);
-        if (plan.mma) return plan.dp == 64 ? launch_mma<64>(wide, a, st) : plan.dp == 128 ? launch_mma<128>(wide, a, st) : launch_mma<256>(wide, a, st);
-        if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3((unsigned)a.items), 128, attend_simt_bytes(p.dim), st, a);
-        return launch_dependent<k_attend_simt<float>>(dim3((unsigned)a.items), 128, attend_simt_bytes(p.dim), st, a);
+        a.with_prefix = prefix;
+        a.with_own = own;
+        a.here = own ? p.own : p.prefix;
+        if (plan.mma) return p.dim <= 64 ? launch_mma<64>(a, st) : p.dim <= 128 ? launch_mma<128>(a, st) : launch_mma<256>(a, st);
+        if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
+        return launch_dependent<k_attend_simt<float>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
     };
-    if (p.tc.ctas > 0 && (rc = launch_prefix_tc(p, st)) != METEORA_OK) return rc;
-    if (plan.wide[0] == plan.wide[1]) {
-        rc = pieces(prefix_items, own_items, plan.wide[0]);
-    } else {
-        rc = pieces(prefix_items, 0, plan.wide[0]);
-        if (rc == METEORA_OK) rc = pieces(0, own_items, plan.wide[1]);
-    }
+    int rc = METEORA_OK;
+    if (z.prefix_len > 0 && !plan.together) rc = p.tc ? launch_prefix_tc(p, st) : pieces(true, false);
+    if (rc == METEORA_OK) rc = pieces(plan.together, true);
     if (rc != METEORA_OK) return rc;
-    const long long join = ((long long)z.T * z.q_heads + 3) / 4;
-    if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_join<__nv_bfloat16>>(dim3((unsigned)join), 128, 0, st, p);
-    return launch_dependent<k_attend_join<float>>(dim3((unsigned)join), 128, 0, st, p);
+    return z.dtype == METEORA_BF16 ? launch_join<__nv_bfloat16>(p, st) : launch_join<float>(p, st);
 }
 
 }  // namespace meteora

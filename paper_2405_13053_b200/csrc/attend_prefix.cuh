@@ -1,9 +1,8 @@
 // The shared prefix of a bf16 batch on the tensor cores: rows of all sequences against the prefix's keys (attend.cuh has
 // the mathematics and where the pieces go).  Included by wgemm_tcgen05.cu after the device helpers it uses.
 //
-// A unit of work is 256 rows (token, head of one kv head's group) x the prefix, in tiles of 128 keys.  The units' tiles are
-// dealt to the CTAs in even shares, one after the other, so that no SM idles behind an uneven number of units; a share that
-// starts or ends inside a unit leaves its part as a piece (prefix_pieces tells the join how many a row has).
+// A unit of work is 256 rows (token, head of one kv head's group) x the prefix, in tiles of 128 keys; the tiles are dealt to
+// one CTA per SM in even shares (units of one kv head follow one another: their CTAs read the same keys at about the same time).
 //
 // The rows are two tiles of 128 with a softmax group of four warps each, one thread per row.  Scores S = Q K^T go to TMEM,
 // the group turns them into weights 2^(s - m), rounded to bf16 and stored over the scores they came from, and the second
@@ -21,8 +20,7 @@
 
 namespace meteora {
 
-constexpr int kPfxKeys = 128;                        // keys per tile
-constexpr int kPfxRows = kPrefixRows;                // rows per unit
+constexpr int kPfxKeys = kPrefixTile, kPfxRows = kPrefixRows;
 constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
 
 template <int D> struct PrefixShape {
@@ -100,8 +98,9 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8);
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8 + kPfxMasks * 4);
     const int warp = warp_id(), lane = threadIdx.x & 31;
-    const PrefixShare sh = p.tc;
-    const long long x_lo = share_start(sh, blockIdx.x), x_hi = share_start(sh, blockIdx.x + 1);
+    const int unit_tiles = (p.batch.prefix + kPfxKeys - 1) / kPfxKeys;
+    const Shares shares((uint32_t)p.prefix.total, gridDim.x);
+    const int x_lo = (int)shares.start(blockIdx.x), x_hi = (int)shares.start(blockIdx.x + 1);
     const int rows_all = p.batch.T * p.group, pair_tiles = (rows_all + kPfxRows - 1) / kPfxRows;
 
     if (threadIdx.x == 0) {
@@ -136,8 +135,8 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     if (warp == 0) {
         // ---- copies: K then V of every tile, page by page
         int n = 0, tails = 0, done = 0;
-        for (long long x = x_lo; x < x_hi && ok; ++x, ++done) {
-            const int unit = (int)(x / sh.tiles), tile = (int)(x - (long long)unit * sh.tiles), h = unit / pair_tiles;
+        for (int x = x_lo; x < x_hi && ok; ++x, ++done) {
+            const int unit = x / unit_tiles, tile = x - unit * unit_tiles, h = unit / pair_tiles;
             const int key0 = tile * kPfxKeys, boxes = kPfxKeys >> pp.box_shift;
             const int limit = min(kPfxKeys, p.batch.prefix - key0);            // keys of the tile that there are
             long long page = -1;
@@ -221,9 +220,9 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             __syncwarp();
         };
         auto wait_full = [&](int i) { return mbar_wait_warp(bar_full + (i % S::kStages) * 8, (i / S::kStages) & 1); };
-        for (long long x = x_lo; x < x_hi && ok;) {
-            const int unit = (int)(x / sh.tiles), row0 = unit % pair_tiles * kPfxRows;
-            const int count = (int)(min(x_hi, (long long)(unit + 1) * sh.tiles) - x), active = rows_all - row0 > 128 ? 2 : 1;
+        for (int x = x_lo; x < x_hi && ok;) {
+            const int unit = x / unit_tiles, row0 = unit % pair_tiles * kPfxRows;
+            const int count = min(x_hi, (unit + 1) * unit_tiles) - x, active = rows_all - row0 > 128 ? 2 : 1;
             ok = wait_full(n);
             for (int i = 0; i < active && ok; ++i) ok = mbar_wait_warp(bar_q + i * 8, segs_of[i] & 1);
             if (!ok) {
@@ -266,38 +265,44 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + 256 + i * 128;
         int tiles = 0, segs = 0, done = 0;
-        for (long long x = x_lo; x < x_hi && ok;) {
-            const int unit = (int)(x / sh.tiles), h = unit / pair_tiles, row0 = unit % pair_tiles * kPfxRows;
-            const int count = (int)(min(x_hi, (long long)(unit + 1) * sh.tiles) - x), first_tile = (int)(x - (long long)unit * sh.tiles);
+        for (int x = x_lo; x < x_hi && ok;) {
+            const int unit = x / unit_tiles, h = unit / pair_tiles, row0 = unit % pair_tiles * kPfxRows;
+            const int count = min(x_hi, (unit + 1) * unit_tiles) - x, first_tile = x - unit * unit_tiles;
             if (i == 1 && rows_all - row0 <= 128) {                            // no rows for the second tile
                 x += count;
                 done += count;
                 continue;
             }
-            // queries: each thread its own row
+            // queries: a warp its 32 rows, each row's chunks by neighbouring lanes
             const int row = row0 + i * 128 + r;
             const bool live = row < rows_all;
-            const int t = live ? row / p.group : 0, g = live ? row - t * p.group : 0;
             {
-                const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(h * p.group + g) * p.q_h;
-                const bool wide = ((uintptr_t)src & 15) == 0;
+                constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks;
                 const uint32_t flip = pp.sign < 0 ? 0x80008000u : 0u, keep = pp.sign ? 0xFFFFFFFFu : 0u;
-                uint8_t* const dst = base_ptr + i * S::kTileBytes + r * 128;
+                const int c = lane % kChunks;
+                uint4 v[32 / kAtOnce];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (live) {
-                        if (wide) {
-                            v = *reinterpret_cast<const uint4*>(src + c * 8);
+                for (int q = 0; q < 32 / kAtOnce; ++q) {
+                    const int rr = (warp & 3) * 32 + q * kAtOnce + lane / kChunks, at = row0 + i * 128 + rr;
+                    v[q] = make_uint4(0u, 0u, 0u, 0u);
+                    if (at < rows_all) {
+                        const int t = at / p.group, g = at - t * p.group;
+                        const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(h * p.group + g) * p.q_h + c * 8;
+                        if (((uintptr_t)src & 15) == 0) {
+                            v[q] = *reinterpret_cast<const uint4*>(src);
                         } else {
                             __nv_bfloat16 e[8];
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) e[q] = src[c * 8 + q];
-                            memcpy(&v, e, 16);
+                            for (int x = 0; x < 8; ++x) e[x] = src[x];
+                            memcpy(&v[q], e, 16);
                         }
                     }
-                    v.x = (v.x ^ flip) & keep, v.y = (v.y ^ flip) & keep, v.z = (v.z ^ flip) & keep, v.w = (v.w ^ flip) & keep;
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * (kPfxKeys * 128) + (((c & 7) ^ (r & 7)) << 4)) = v;
+                }
+#pragma unroll
+                for (int q = 0; q < 32 / kAtOnce; ++q) {
+                    const int rr = (warp & 3) * 32 + q * kAtOnce + lane / kChunks;
+                    v[q].x = (v[q].x ^ flip) & keep, v[q].y = (v[q].y ^ flip) & keep, v[q].z = (v[q].z ^ flip) & keep, v[q].w = (v[q].w ^ flip) & keep;
+                    *reinterpret_cast<uint4*>(base_ptr + i * S::kTileBytes + (c >> 3) * (kPfxKeys * 128) + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[q];
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(bar_q + i * 8);
@@ -378,18 +383,28 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 break;
             }
             tc_fence_after();
-            const int slot = (int)blockIdx.x - share_of(sh, (long long)unit * sh.tiles);
-            const size_t out = (size_t)slot * p.batch.T * p.q_heads + (size_t)t * p.q_heads + h * p.group + g;
-            if (live) p.part_ml[out] = make_float2(ref, l);
+            // 32 entries at a time through the place of this warp's queries (32 rows of 128 bytes in either half), so that
+            // a store is whole lines of four rows; a thread's own row straight from its registers takes 32 of them
+            const size_t piece = (size_t)(unit + (int)blockIdx.x) * kPfxRows + i * 128 + (warp & 3) * 32;
+            const int rows_here = min(32, rows_all - row0 - i * 128 - (warp & 3) * 32);
+            if (live) p.prefix.ml[piece + lane] = make_float2(ref, l);
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
                 float o[32];
                 tmem_ld32(t_o + c, o);
                 tmem_wait_ld();
-                if (live)
+                uint8_t* const turn = base_ptr + i * S::kTileBytes + (c / 32 % kHalves) * (kPfxKeys * 128) + (warp & 3) * 4096;
 #pragma unroll
-                    for (int q = 0; q < 32; q += 4)
-                        *reinterpret_cast<float4*>(p.part_o + out * D + c + q) = make_float4(o[q], o[q + 1], o[q + 2], o[q + 3]);
+                for (int q = 0; q < 8; ++q)
+                    *reinterpret_cast<float4*>(turn + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const int rr = q * 4 + (lane >> 3);
+                    const float4 v = *reinterpret_cast<const float4*>(turn + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4));
+                    if (rr < rows_here) *reinterpret_cast<float4*>(p.prefix.o + (piece + rr) * D + c + (lane & 7) * 4) = v;
+                }
+                __syncwarp();
             }
             tc_fence_before();
             mbar_arrive(bar_ofree + i * 8);

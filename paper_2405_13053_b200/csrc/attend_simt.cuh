@@ -1,6 +1,6 @@
 // Pieces of attention on CUDA cores: fp32 caches, and heads whose rows are no whole 16-byte vectors.
 //
-// A CTA of 128 threads takes up to 16 rows and walks a piece's keys in tiles of 64, held in shared memory as fp32.  Scores:
+// A CTA of 128 threads walks its share of the tiles (attend.cuh), units of 16 rows, 64 keys held in shared memory as fp32.  Scores:
 // a thread has two rows and four keys, 32 FMAs for six 16-byte reads.  Weighted sum: a thread has its entries of all rows,
 // one read of a value for 16 FMAs.  A key that a row does not see has weight 0 and is left out of that row's sum, whatever
 // its value holds.
@@ -27,54 +27,42 @@ __global__ void __launch_bounds__(128) k_attend_simt(const __grid_constant__ Att
     float* const s_f = s_p + kAttendTile * 20;                 // [16] factors of the sums so far, then [16] the rows' limits
     long long* const s_off = reinterpret_cast<long long*>(s_f + 32);
     const int tid = threadIdx.x, lane = tid & 31;
-    const AttendItem it = attend_item(p, blockIdx.x);
-    const int rows_used = it.tile_tokens * it.tile_heads;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    for (int i = tid; i < kSimtRows * pitch; i += 128) {
-        const int r = i / pitch, e = i - r * pitch;
-        const int t = it.t0 + r / it.tile_heads, g = it.g0 + r % it.tile_heads;
-        float v = 0.f;
-        if (r < rows_used && t < p.batch.T && g < p.group && e < p.dim)
-            v = to_f32(((const E*)p.q)[t * p.q_t + (int64_t)(it.h * p.group + g) * p.q_h + e]) * p.scale_log2;
-        s_q[i] = v;
-    }
+    Walk w = start_walk<1>(p, 0);
     const int ra = (tid >> 4) * 2, kq = tid & 15;              // rows ra, ra + 1 and keys kq + 16 i
-    int t_seg = it.t0;
-    const int t_end = min(p.batch.T, it.t0 + it.tile_tokens);
-    while (t_seg < t_end) {
-        OwnRange seg = {-1, 0, 0, t_end, it.piece * p.prefix_piece, min(p.batch.prefix, (it.piece + 1) * p.prefix_piece)};
-        if (!it.prefix) {
-            const int b = sequence_of(p.batch, t_seg, lane);
-            if (b < 0) {
-                ++t_seg;
-                continue;
-            }
-            seg = own_range(p, b, it.piece, t_seg, t_end);
+    while (w.left > 0) {
+        const Walk u = w;                                      // the unit at hand
+        const int rows_used = (int)min((long long)kSimtRows, (long long)u.tokens * p.group - (long long)u.rt * kSimtRows);
+        __syncthreads();
+        for (int i = tid; i < kSimtRows * pitch; i += 128) {
+            const int r = i / pitch, e = i - r * pitch;
+            int t, g;
+            float v = 0.f;
+            if (e < p.dim && row_place(p, u, r, t, g))
+                v = to_f32(((const E*)p.q)[t * p.q_t + (int64_t)(u.h * p.group + g) * p.q_h + e]) * p.scale_log2;
+            s_q[i] = v;
         }
-        if (seg.lo >= seg.hi) {
-            t_seg = seg.t_next;
-            continue;
-        }
-        const PageList pages = page_list(p.batch, seg.b);
-        int lim[2];
+        const PageList pages = page_list(p.batch, u.b);
+        int lim[2], t0, g0;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int t = it.t0 + (ra + i) / it.tile_heads;
-            const bool mine = ra + i < rows_used && t >= t_seg && t < seg.t_next;
-            lim[i] = !mine ? 0 : it.prefix ? seg.hi : own_limit(seg, t);
+            int t, g;
+            lim[i] = row_place(p, u, ra + i, t, g) ? row_limit(u, t) : 0;
         }
-        __syncthreads();
         if (kq == 0) reinterpret_cast<int2*>(s_f + 16)[ra / 2] = make_int2(lim[0], lim[1]);
-        const int lim_all = it.prefix ? seg.hi : own_limit(seg, t_seg);
+        row_place(p, u, 0, t0, g0);
+        const int lim_all = row_limit(u, t0);
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[2][kSimtRows];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int r = 0; r < kSimtRows; ++r) o[i][r] = 0.f;
-        for (int key0 = seg.lo; key0 < seg.hi; key0 += kAttendTile) {
+        bool more = true;
+        while (more) {
+            const int key0 = w.tile * kAttendTile;
             __syncthreads();
-            if (tid < kAttendTile) s_off[tid] = key0 + tid < seg.hi ? key_row(pages, p.batch, key0 + tid, p.kv_heads, it.h) : -1ll;
+            if (tid < kAttendTile) s_off[tid] = key0 + tid < u.hi ? key_row(pages, p.batch, p.by_page, key0 + tid, p.kv_heads, u.h) : -1ll;
             __syncthreads();
             if (sizeof(E) == 4 && p.dim % 4 == 0) {
                 for (int i = tid; i < kAttendTile * quads; i += 128) {
@@ -137,7 +125,7 @@ __global__ void __launch_bounds__(128) k_attend_simt(const __grid_constant__ Att
                 }
             }
             __syncthreads();
-            const int n = min(kAttendTile, seg.hi - key0);
+            const int n = min(kAttendTile, u.hi - key0);
             const bool masked = key0 + kAttendTile > lim_all;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -176,35 +164,26 @@ __global__ void __launch_bounds__(128) k_attend_simt(const __grid_constant__ Att
                     o[i][4 * q + 3] = a.w;
                 }
             }
+            more = w.next(p) && w.unit == u.unit;
         }
-        const size_t all_rows = (size_t)p.batch.T * p.q_heads;
-        auto out_row = [&](int r, bool& mine) {
-            const int t = it.t0 + r / it.tile_heads, g = it.g0 + r % it.tile_heads;
-            mine = r < rows_used && t >= t_seg && t < seg.t_next && g < p.group;
-            return (size_t)it.slot * all_rows + (size_t)t * p.q_heads + it.h * p.group + g;
-        };
+        if (u.unit + (int)blockIdx.x >= p.here.pieces) continue;
+        const size_t piece = (size_t)(u.unit + (int)blockIdx.x) * kSimtRows;
         const unsigned peers = 0xFFFFu << (lane & 16);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float sum = l[j];
 #pragma unroll
             for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(peers, sum, x);
-            bool mine;
-            const size_t row = out_row(ra + j, mine);
-            if (mine && kq == 0) p.part_ml[row] = make_float2(m[j], sum);
+            if (ra + j < rows_used && kq == 0) p.here.ml[piece + ra + j] = make_float2(m[j], sum);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = tid + 128 * i;
             if (e >= p.dim) continue;
 #pragma unroll
-            for (int r = 0; r < kSimtRows; ++r) {
-                bool mine;
-                const size_t row = out_row(r, mine);
-                if (mine) p.part_o[row * p.dim + e] = o[i][r];
-            }
+            for (int r = 0; r < kSimtRows; ++r)
+                if (r < rows_used) p.here.o[(piece + r) * p.dim + e] = o[i][r];
         }
-        t_seg = seg.t_next;
     }
 }
 

@@ -11,8 +11,8 @@ namespace meteora {
 template <auto kernel, typename... A>
 int launch_dependent(dim3 grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
     if (smem > 48 * 1024) {
-        static std::atomic<bool> allowed[64];                       // per device; always the device's largest, for all sizes at once
-        constexpr int kMaxSmem = 227 * 1024;
+        static std::atomic<bool> allowed[64];                       // per device; one size for all launches (the rest of 227 KB is for static arrays)
+        constexpr int kMaxSmem = 226 * 1024;
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e == cudaSuccess && (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed))) {
@@ -64,6 +64,8 @@ struct AttendSizes {
 // wgemm_tcgen05.cu: the prefix on the tensor cores
 bool prefix_tc_supported(const AttendSizes& z);
 int launch_prefix_tc(const AttendParams& p, cudaStream_t st);
+// and units of up to 16 rows (entries of a head padded to `padded`: 64, 128 or 256)
+int launch_attend_warp(const AttendParams& p, int padded, cudaStream_t st);
 size_t attend_workspace_bytes(const AttendSizes& z);
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,
                             const BatchView& batch, const AttendSizes& z, float scale, void* workspace, cudaStream_t st);

@@ -760,6 +760,7 @@ k_wgemm(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ CUtens
 #include "gate_dwg.cuh"
 #include "expand_tile.cuh"
 #include "attend_prefix.cuh"
+#include "attend_warp.cuh"
 
 namespace meteora {
 
@@ -3075,7 +3076,7 @@ static int get_cache_map(const void* ptr, int D, int page_size, long long planes
 
 template <int D>
 static int launch_prefix_tc_d(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixTcParams& pp, cudaStream_t st) {
-    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.tc.ctas), kThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
+    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.prefix.workers), kThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
 }
 
 int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
@@ -3090,6 +3091,26 @@ int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
     if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tk)) != METEORA_OK) return rc;
     if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tv)) != METEORA_OK) return rc;
     return p.dim == 64 ? launch_prefix_tc_d<64>(tk, tv, pp, st) : launch_prefix_tc_d<128>(tk, tv, pp, st);
+}
+
+template <int DP, bool kTma>
+static int launch_attend_warp_d(const AttendParams& p, int box_rows, cudaStream_t st) {
+    CUtensorMap tk = {}, tv = {};
+    int rc, shift = 0;
+    if (kTma) {
+        if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, &tk)) != METEORA_OK) return rc;
+        if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, &tv)) != METEORA_OK) return rc;
+        while ((1 << shift) < box_rows) ++shift;
+    }
+    return launch_dependent<k_attend_warp<DP, kTma>>(dim3(p.here.workers / 4), 128, AttendWarpShape<DP>::kBytes, st, tk, tv, p, shift);
+}
+
+int launch_attend_warp(const AttendParams& p, int padded, cudaStream_t st) {
+    const int box_rows = std::min(kWarpTile, prefix_box_rows(p.batch.page));
+    const bool tma = box_rows >= 8 && p.dim == padded && p.batch.n_pages > 0 && p.batch.n_pages * p.kv_heads < (1LL << 31);
+    if (padded == 64) return tma ? launch_attend_warp_d<64, true>(p, box_rows, st) : launch_attend_warp_d<64, false>(p, box_rows, st);
+    if (padded == 128) return tma ? launch_attend_warp_d<128, true>(p, box_rows, st) : launch_attend_warp_d<128, false>(p, box_rows, st);
+    return tma ? launch_attend_warp_d<256, true>(p, box_rows, st) : launch_attend_warp_d<256, false>(p, box_rows, st);
 }
 
 // Knob wait_limit_us: the limit of the bounded device-side waits on the current device (0: the default, about a second).
