@@ -201,8 +201,8 @@ struct Walk {
     }
 };
 
-// The start of a worker's share, worked out by its CTA of 128 threads and kWorkers workers (this thread's is `mine`).  CTA 0
-// leaves the totals and the sequences' starts for the join.
+// The start of a worker's share, worked out by its CTA of 128 threads and kWorkers workers (this thread's is `mine`).  For the
+// join CTA 0 leaves the totals, and whoever has a sequence's first tile its start.
 template <int kWorkers>
 __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
     constexpr int kThreadsOf = 128, kWarps = kThreadsOf / 32;
@@ -260,12 +260,12 @@ __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
         if (p.with_own) p.total[1] = (int)W;
     }
     if (tid < kWorkers && start(c0 + tid) < before) s_b[tid] = -1, s_x[tid] = 0, s_unit[tid] = 0;
-    if (blockIdx.x == 0 || (x < start(c0 + kWorkers) && x + min(tiles, kMost) > start(c0))) {
+    if (x < start(c0 + kWorkers) && x + min(tiles, kMost) > start(c0)) {
         for (int b = b_lo; b < b_hi; ++b) {
             w.enter(p, b);
             if (w.tiles == 0 || w.n_rt == 0) continue;
             const uint32_t n = (uint32_t)(w.n_rt * p.kv_heads) * (uint32_t)w.tiles;
-            if (blockIdx.x == 0) p.first_tile[b] = (int)x, p.first_unit[b] = u;
+            if (x >= start(c0) && x < start(c0 + kWorkers)) p.first_tile[b] = (int)x, p.first_unit[b] = u;
 #pragma unroll
             for (int i = 0; i < kWorkers; ++i) {
                 const uint32_t lo = start(c0 + i);

@@ -39,7 +39,7 @@ template <int DP> struct AttendWarpShape {
     static constexpr int kStages = 3;
     static constexpr int kInfos = 4;                               // tiles described: one more than kStages
     static constexpr int kWarpBytes = 2 * kStages * kTileBytes;
-    static constexpr int kBytes = 1024 + 4 * (kWarpBytes + kInfos * 48 + kStages * 8);
+    static constexpr int kBytes = 1024 + 4 * (kWarpBytes + kInfos * 40 + kStages * 8);
 };
 
 }  // namespace meteora

@@ -4,13 +4,16 @@
 // A unit of work is 256 rows (token, head of one kv head's group) x the prefix, in tiles of 128 keys; the tiles are dealt to
 // one CTA per SM in even shares (units of one kv head follow one another: their CTAs read the same keys at about the same time).
 //
-// The rows are two tiles of 128 with a softmax group of four warps each, one thread per row.  Scores S = Q K^T go to TMEM,
-// the group turns them into weights 2^(s - m), rounded to bf16 and stored over the scores they came from, and the second
-// product O += P V takes P from there (A operand in TMEM) and V as it lies (its entries contiguous: the MN-major form of B).
-// While one group works on its scores the tensor core has the other tile's products: S and PV of a tile are 512 cycles
-// each (128 x 128 x 128), a tile's 16384 exponentials 1024 at 16 per cycle, so at 256 rows tensor core and exponentials
-// are nearly even.  A row's reference m is not its running maximum: it stays until the maximum is 8 above it, which
-// leaves weights below 2^8 and spares nearly all rescaling of O.
+// The rows are two tiles of 128 with a softmax group of eight warps each, two threads per row, 64 of a tile's keys each.
+// Scores S = Q K^T go to TMEM, the group turns them into weights 2^(s - m), rounded to bf16 and stored over the scores they
+// came from, and the second product O += P V takes P from there (A operand in TMEM) and V as it lies (its entries
+// contiguous: the MN-major form of B).  While one group works on its scores the tensor core has the other tile's products:
+// S and PV of a tile are 512 cycles each (128 x 128 x 128), a tile's 16384 exponentials 1024 at 16 per cycle, so at 256
+// rows tensor core and exponentials are nearly even.  (One thread per row, four warps to a group: 5600 cycles a tile of 256
+// rows; two warps per scheduler hide little of each other's latency.)
+// A row's reference m is not its running maximum: it stays until the maximum is 8 above it, which leaves weights below 2^8
+// and spares nearly all rescaling of O.  The two threads of a row need the same m: their warps exchange one word that says
+// whether any of their rows needs a new one, and only then the maxima themselves (through unused columns of TMEM).
 //
 // A page that is not there and the keys behind the prefix's end count as -inf, and their values are zeroed in shared memory:
 // what the cache holds there (an infinity, a NaN) would pass a weight of 0.
@@ -21,13 +24,15 @@
 namespace meteora {
 
 constexpr int kPfxKeys = kPrefixTile, kPfxRows = kPrefixRows;
+constexpr int kPfxThreads = 576;                     // warp 0: copies, warp 1: products, 16 warps of softmax
 constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
 
 template <int D> struct PrefixShape {
     static constexpr int kTileBytes = kPfxKeys * D * 2;
     static constexpr int kStages = D == 128 ? 5 : 11;              // of keys or values of one tile
     static constexpr int kBarOff = (2 + kStages) * kTileBytes;     // barriers, then page masks, TMEM slot
-    static constexpr int kSmem = 1024 + kBarOff + (2 * kStages + 11) * 8 + kPfxMasks * 4 + 16;
+    static constexpr int kBars = 2 * kStages + 19;
+    static constexpr int kSmem = 1024 + kBarOff + kBars * 8 + kPfxMasks * 4 + 16 * 4 + 16;
 };
 
 struct PrefixTcParams {
@@ -58,6 +63,20 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    return __uint_as_float(r);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -84,7 +103,7 @@ __device__ __forceinline__ unsigned long long fma2_of(unsigned long long a, unsi
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kPfxThreads, 1)
 k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixTcParams pp) {
     typedef PrefixShape<D> S;
     constexpr int kHalves = D / 64;
@@ -94,9 +113,10 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     uint8_t* const base_ptr = smem_raw + (base - raw);
     const uint32_t s_q = base, ring = base + 2 * S::kTileBytes;
     const uint32_t bar_full = base + S::kBarOff, bar_free = bar_full + S::kStages * 8, bar_s = bar_free + S::kStages * 8, bar_p = bar_s + 16,
-                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_tail = bar_q + 16;
-    volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8);
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kBarOff + (2 * S::kStages + 11) * 8 + kPfxMasks * 4);
+                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_x = bar_q + 16, bar_tail = bar_x + 64;
+    volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kBarOff + S::kBars * 8);
+    volatile uint32_t* const s_grow = s_mask + kPfxMasks;          // [tile of rows][half][quarter]
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kBarOff + S::kBars * 8 + kPfxMasks * 4 + 16 * 4);
     const int warp = warp_id(), lane = threadIdx.x & 31;
     const int unit_tiles = (p.batch.prefix + kPfxKeys - 1) / kPfxKeys;
     const Shares shares((uint32_t)p.prefix.total, gridDim.x);
@@ -110,11 +130,12 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_s + i * 8, 1);
-            mbar_init(bar_p + i * 8, 128);
+            mbar_init(bar_p + i * 8, 8);
             mbar_init(bar_o + i * 8, 1);
-            mbar_init(bar_ofree + i * 8, 128);
-            mbar_init(bar_q + i * 8, 128);
+            mbar_init(bar_ofree + i * 8, 8);
+            mbar_init(bar_q + i * 8, 8);
         }
+        for (int i = 0; i < 8; ++i) mbar_init(bar_x + i * 8, 2);
         mbar_init(bar_tail, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -165,7 +186,7 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                     const CUtensorMap* tm = which ? &tmV : &tmK;
 #pragma unroll
                     for (int c = 0; c < kHalves; ++c)
-                        tma_load_3d(dst + c * (kPfxKeys * 128) + lane * pp.box_rows * 128, tm, c * 64, at, (int)page * p.kv_heads + h, bar);
+                        tma_load_4d(dst + c * (kPfxKeys * 128) + lane * pp.box_rows * 128, tm, 0, at, c, (int)page * p.kv_heads + h, bar);
                 }
                 __syncwarp();
                 if (slow) {
@@ -260,11 +281,23 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             x += count;
         }
     } else {
-        // ---- softmax: warps 2 - 5 have the first 128 rows, 6 - 9 the second; a warp's TMEM lanes are those of its number mod 4
-        const int i = warp >= 6, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        // ---- softmax: four groups of four warps, (tile of rows, half of the keys); a warp's TMEM lanes are those of its number mod 4
+        const int i = (warp - 2) >> 3, half = (warp - 2) >> 2 & 1, quad = warp & 3;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + 256 + i * 128;
-        int tiles = 0, segs = 0, done = 0;
+        const uint32_t bar_pair = bar_x + (i * 4 + quad) * 8;
+        volatile uint32_t* const grow_mine = s_grow + (i * 2 + half) * 4 + quad;
+        volatile uint32_t* const grow_other = s_grow + (i * 2 + 1 - half) * 4 + quad;
+        constexpr int kCols = kPfxKeys / 2, kPart = D / 4;         // scores of a thread; entries of O that leave at a time
+        int tiles = 0, segs = 0, done = 0, pairs = 0;
+        // The two warps of 32 rows wait for each other.
+        auto meet = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_pair);
+            const bool met = mbar_wait_warp(bar_pair, pairs & 1);
+            ++pairs;
+            return met;
+        };
         for (int x = x_lo; x < x_hi && ok;) {
             const int unit = x / unit_tiles, h = unit / pair_tiles, row0 = unit % pair_tiles * kPfxRows;
             const int count = min(x_hi, (unit + 1) * unit_tiles) - x, first_tile = x - unit * unit_tiles;
@@ -273,89 +306,102 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 done += count;
                 continue;
             }
-            // queries: a warp its 32 rows, each row's chunks by neighbouring lanes
-            const int row = row0 + i * 128 + r;
-            const bool live = row < rows_all;
+            // queries: a warp 16 of the 32 rows, each row's chunks by neighbouring lanes
             {
                 constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks;
                 const uint32_t flip = pp.sign < 0 ? 0x80008000u : 0u, keep = pp.sign ? 0xFFFFFFFFu : 0u;
                 const int c = lane % kChunks;
-                uint4 v[32 / kAtOnce];
+                uint4 v[16 / kAtOnce];
 #pragma unroll
-                for (int q = 0; q < 32 / kAtOnce; ++q) {
-                    const int rr = (warp & 3) * 32 + q * kAtOnce + lane / kChunks, at = row0 + i * 128 + rr;
+                for (int q = 0; q < 16 / kAtOnce; ++q) {
+                    const int at = row0 + i * 128 + quad * 32 + half * 16 + q * kAtOnce + lane / kChunks;
                     v[q] = make_uint4(0u, 0u, 0u, 0u);
                     if (at < rows_all) {
-                        const int t = at / p.group, g = at - t * p.group;
+                        const int t = (int)p.by_group.of((unsigned)at), g = at - t * p.group;
                         const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(h * p.group + g) * p.q_h + c * 8;
                         if (((uintptr_t)src & 15) == 0) {
                             v[q] = *reinterpret_cast<const uint4*>(src);
                         } else {
                             __nv_bfloat16 e[8];
 #pragma unroll
-                            for (int x = 0; x < 8; ++x) e[x] = src[x];
+                            for (int y = 0; y < 8; ++y) e[y] = src[y];
                             memcpy(&v[q], e, 16);
                         }
                     }
                 }
 #pragma unroll
-                for (int q = 0; q < 32 / kAtOnce; ++q) {
-                    const int rr = (warp & 3) * 32 + q * kAtOnce + lane / kChunks;
+                for (int q = 0; q < 16 / kAtOnce; ++q) {
+                    const int rr = quad * 32 + half * 16 + q * kAtOnce + lane / kChunks;
                     v[q].x = (v[q].x ^ flip) & keep, v[q].y = (v[q].y ^ flip) & keep, v[q].z = (v[q].z ^ flip) & keep, v[q].w = (v[q].w ^ flip) & keep;
                     *reinterpret_cast<uint4*>(base_ptr + i * S::kTileBytes + (c >> 3) * (kPfxKeys * 128) + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[q];
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(bar_q + i * 8);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_q + i * 8);
             }
             float ref = -INFINITY, l = 0.f;
             for (int j = 0; j < count; ++j, ++tiles, ++done) {
-                ok = mbar_wait(bar_s + i * 8, tiles & 1);
-                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                if (!mbar_wait_warp(bar_s + i * 8, tiles & 1)) {
                     ok = false, where = 5;
                     break;
                 }
                 tc_fence_after();
                 const uint32_t mask = s_mask[done % kPfxMasks];
-                const int limit = min(kPfxKeys, p.batch.prefix - (first_tile + j) * kPfxKeys);
-                float s[kPfxKeys];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, s + c * 32);
+                const int limit = min(kPfxKeys, p.batch.prefix - (first_tile + j) * kPfxKeys) - half * kCols;
+                float s[kCols];
+                tmem_ld32(t_s + half * kCols, s);
+                tmem_ld32(t_s + half * kCols + 32, s + 32);
                 tmem_wait_ld();
-                if (limit < kPfxKeys || __popc(mask) < (kPfxKeys >> pp.box_shift)) {
+                if (limit < kCols || __popc(mask) < (kPfxKeys >> pp.box_shift)) {
 #pragma unroll
-                    for (int k = 0; k < kPfxKeys; ++k)
-                        if (k >= limit || !(mask >> (k >> pp.box_shift) & 1u)) s[k] = -INFINITY;
+                    for (int k = 0; k < kCols; ++k)
+                        if (k >= limit || !(mask >> ((half * kCols + k) >> pp.box_shift) & 1u)) s[k] = -INFINITY;
                 }
-                float top[4] = {s[0], s[1], s[2], s[3]};
+                float top[2] = {max3(s[0], s[2], s[4]), max3(s[1], s[3], s[5])};
 #pragma unroll
-                for (int k = 4; k < kPfxKeys; k += 4)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) top[q] = fmaxf(top[q], s[k + q]);
-                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
-                const bool grow = high > ref + 8.f || (ref == -INFINITY && high > -INFINITY);
-                if (j > 0 && __any_sync(0xFFFFFFFFu, grow)) {
+                for (int k = 6; k + 3 < kCols; k += 4) {
+                    top[0] = max3(top[0], s[k], s[k + 2]);
+                    top[1] = max3(top[1], s[k + 1], s[k + 3]);
+                }
+                float high = max3(top[0], top[1], fmaxf(s[kCols - 2], s[kCols - 1])) * p.scale_log2;
+                bool grow = high > ref + 8.f || (ref == -INFINITY && high > -INFINITY);
+                const bool any = __any_sync(0xFFFFFFFFu, grow);
+                if (lane == 0) *grow_mine = any;
+                tc_fence_before();
+                ok = meet();                                                   // (and both have their scores: the weights may take their place)
+                tc_fence_after();
+                if (ok && (any || *grow_other)) {                              // (the same on both sides)
+                    tmem_st1(t_s + 64 + half, high);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    ok = meet();
+                    tc_fence_after();
+                    high = fmaxf(high, tmem_ld1(t_s + 65 - half));
+                    grow = high > ref + 8.f || (ref == -INFINITY && high > -INFINITY);
                     const float f = grow ? exp2_fast(ref - high) : 1.f;
                     l *= f;
+                    if (j > 0 && ok) {                                         // this half of the entries of O
 #pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        float o[32];
-                        tmem_ld32(t_o + c, o);
-                        tmem_wait_ld();
-                        uint32_t w[16];
+                        for (int c = 0; c < D / 2; c += 16) {
+                            uint32_t w[16];
+                            float o[16];
+                            tmem_ld16(t_o + half * (D / 2) + c, o);
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-#pragma unroll
-                            for (int q = 0; q < 16; ++q) w[q] = __float_as_uint(o[hh * 16 + q] * f);
-                            tmem_st16(t_o + c + hh * 16, w);
+                            for (int q = 0; q < 16; ++q) w[q] = __float_as_uint(o[q] * f);
+                            tmem_st16(t_o + half * (D / 2) + c, w);
                         }
                     }
+                    if (grow) ref = high;
                 }
-                if (grow) ref = high;
+                if (!ok) {
+                    where = 7;
+                    break;
+                }
                 const float m = ref == -INFINITY ? 0.f : ref;
                 const unsigned long long sc2 = pair2(p.scale_log2, p.scale_log2), m2 = pair2(-m, -m);
                 unsigned long long sum2[2] = {0ull, 0ull};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t w[16];
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
@@ -366,7 +412,7 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(b), "f"(a));
                         add2(sum2[q & 1], bf16x2_to_f32x2(w[q]));
                     }
-                    tmem_st16(t_s + c * 16, w);
+                    tmem_st16(t_s + half * 32 + c * 16, w);
                 }
                 add2(sum2[0], sum2[1]);
                 float a, b;
@@ -374,40 +420,60 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 l += a + b;
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(bar_p + i * 8);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_p + i * 8);
             }
             if (!ok) break;
-            ok = mbar_wait(bar_o + i * 8, segs & 1);
-            if (!__all_sync(0xFFFFFFFFu, ok)) {
+            if (!mbar_wait_warp(bar_o + i * 8, segs & 1)) {
                 ok = false, where = 6;
                 break;
             }
             tc_fence_after();
-            // 32 entries at a time through the place of this warp's queries (32 rows of 128 bytes in either half), so that
-            // a store is whole lines of four rows; a thread's own row straight from its registers takes 32 of them
-            const size_t piece = (size_t)(unit + (int)blockIdx.x) * kPfxRows + i * 128 + (warp & 3) * 32;
-            const int rows_here = min(32, rows_all - row0 - i * 128 - (warp & 3) * 32);
-            if (live) p.prefix.ml[piece + lane] = make_float2(ref, l);
+            // kPart entries at a time through the place of the queries, so that a store is whole lines of several rows; a
+            // thread's own row straight from its registers takes 32 of them
+            const size_t piece = (size_t)(unit + (int)blockIdx.x) * kPfxRows + i * 128 + quad * 32;
+            const int rows_here = min(32, rows_all - row0 - i * 128 - quad * 32);
+            // the row's sum: the halves' sums through a column of TMEM that no product uses any more
+            if (half == 1) {
+                tmem_st1(t_s + 64, l);
+                tmem_wait_st();
+            }
+            tc_fence_before();
+            if (!meet()) {
+                ok = false, where = 8;
+                break;
+            }
+            tc_fence_after();
+            if (half == 0) {
+                l += tmem_ld1(t_s + 64);
+                if (lane < rows_here) p.prefix.ml[piece + lane] = make_float2(ref, l);
+            }
+            uint8_t* const turn = base_ptr + i * S::kTileBytes + (D == 128 ? half * (kPfxKeys * 128) : half * 2048) + quad * 4096;
+            constexpr int kQuads = kPart / 4, kRowsAtOnce = 32 / kQuads;       // 16-byte pieces of a row
 #pragma unroll
-            for (int c = 0; c < D; c += 32) {
-                float o[32];
-                tmem_ld32(t_o + c, o);
-                tmem_wait_ld();
-                uint8_t* const turn = base_ptr + i * S::kTileBytes + (c / 32 % kHalves) * (kPfxKeys * 128) + (warp & 3) * 4096;
+            for (int c = 0; c < D / 2; c += kPart) {
+                float o[kPart];
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    *reinterpret_cast<float4*>(turn + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                for (int q = 0; q < kPart; q += 16) tmem_ld16(t_o + half * (D / 2) + c + q, *reinterpret_cast<float(*)[16]>(o + q));
+#pragma unroll
+                for (int q = 0; q < kQuads; ++q)
+                    *reinterpret_cast<float4*>(turn + lane * (kPart * 4) + ((q ^ (lane & (kQuads - 1))) << 4)) =
+                        make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
                 __syncwarp();
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int rr = q * 4 + (lane >> 3);
-                    const float4 v = *reinterpret_cast<const float4*>(turn + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4));
-                    if (rr < rows_here) *reinterpret_cast<float4*>(p.prefix.o + (piece + rr) * D + c + (lane & 7) * 4) = v;
+                for (int q = 0; q < kQuads; ++q) {
+                    const int rr = q * kRowsAtOnce + lane / kQuads, e = lane % kQuads;
+                    const float4 v = *reinterpret_cast<const float4*>(turn + rr * (kPart * 4) + ((e ^ (rr & (kQuads - 1))) << 4));
+                    if (rr < rows_here) *reinterpret_cast<float4*>(p.prefix.o + (piece + rr) * D + half * (D / 2) + c + e * 4) = v;
                 }
                 __syncwarp();
             }
             tc_fence_before();
-            mbar_arrive(bar_ofree + i * 8);
+            if (!meet()) {                                                     // (the other half's queries may take this one's place)
+                ok = false, where = 9;
+                break;
+            }
+            if (lane == 0) mbar_arrive(bar_ofree + i * 8);
             ++segs;
             x += count;
         }

@@ -28,9 +28,10 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     const uint32_t raw = smem_u32(smem_raw), base0 = (raw + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base0 - raw);
     uint8_t* const ring = smem + warp * S::kWarpBytes;             // [stage][K, V][entries / 64][16 keys][128 bytes], chunks swizzled by key
-    int4* const s_info = reinterpret_cast<int4*>(smem + 4 * S::kWarpBytes) + warp * S::kInfos * 3;
+    int4* const s_units = reinterpret_cast<int4*>(smem + 4 * S::kWarpBytes) + warp * S::kInfos * 2;
+    int2* const s_tiles = reinterpret_cast<int2*>(smem + 4 * (S::kWarpBytes + S::kInfos * 32)) + warp * S::kInfos;
     const uint32_t ring0 = base0 + warp * S::kWarpBytes;
-    const uint32_t bar = base0 + 4 * (S::kWarpBytes + S::kInfos * 48) + warp * S::kStages * 8;
+    const uint32_t bar = base0 + 4 * (S::kWarpBytes + S::kInfos * 40) + warp * S::kStages * 8;
     if (kTma && lane == 0) {
 #pragma unroll
         for (int i = 0; i < S::kStages; ++i) mbar_init(bar + i * 8, 1);
@@ -46,77 +47,124 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     auto swz = [](int row, int chunk) { return (uint32_t)((chunk >> 3) * (kWarpTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)); };
     constexpr int kCopies = kWarpTile * S::kChunks / 32;           // 16-byte copies of a lane, for keys and values each
 
-    // A tile is asked for (its description to shared memory, its page number or its keys' places to a register of the
-    // lanes that need them), fetched an iteration later, and used when it has arrived.
-    int asked = 0, fetched = 0;
+    // A tile is asked for (its page numbers or its keys' places are under way), fetched an iteration later, and used when it has
+    // arrived.  What a fetch needs stays in registers, and nothing in it waits; what the use needs goes through shared
+    // memory: a line per tile, and one per unit when it starts.
+    struct Asked {
+        int page0, page1;          // kTma: pages of the tile's halves (one where a page holds both), not looked at yet
+        int in_page;               // kTma: its first key in page0
+        long long place;           // else: of key `lane`
+        int key0, keys, h;
+        bool real, fresh;
+    };
+    int asked = 0, fetched = 0, units = 0;
     bool fresh = true, more = true;
+    int slot = 0, in_page = 0, page = -1;                          // of the tile asked for last, where a page holds whole tiles
+    PageList pages = {};
     auto ask = [&]() {
-        long long found = -1;
-        if (!more) return found;
-        const int key0 = w.tile * kWarpTile, keys = min(kWarpTile, w.hi - key0);
-        const PageList pages = page_list(p.batch, w.b);
-        if (kTma) {                                                // lane i: the page of box i
-            const int key = key0 + (lane << box_shift);
-            const unsigned slot = p.by_page.of((unsigned)key);
-            if ((lane << box_shift) < keys && (int)slot < pages.n) {
-                const int page = __ldg(pages.pages + slot);
-                if (page >= 0 && page < p.batch.n_pages) found = page;
+        Asked a;
+        a.real = more;
+        a.page0 = a.page1 = -1;
+        a.place = -1;
+        if (!more) return a;
+        a.key0 = w.tile * kWarpTile;
+        a.keys = min(kWarpTile, w.hi - a.key0);
+        a.h = w.h;
+        a.fresh = fresh;
+        if (fresh) {
+            pages = page_list(p.batch, w.b);
+            slot = (int)p.by_page.of((unsigned)a.key0);
+            in_page = a.key0 - slot * p.batch.page;
+            ++units;
+            if (lane == 0) {
+                int4* const q = s_units + units % S::kInfos * 2;
+                q[0] = make_int4(w.b, w.rt, w.h, w.first);
+                q[1] = make_int4(w.tokens, w.held, w.hi, w.unit);
             }
-        } else if (lane < keys) {
-            found = key_row(pages, p.batch, p.by_page, key0 + lane, p.kv_heads, w.h);
         }
-        int4* const q = s_info + asked % S::kInfos * 3;
-        const int4 info0 = make_int4(key0, w.hi, 0, w.unit), info1 = make_int4(w.b, w.rt, w.h, w.first);
-        int4 info2 = make_int4(w.tokens, w.held, fresh, 0);
-        const int unit = w.unit;
-        more = w.next(p);
-        fresh = !more || w.unit != unit;
-        info2.w = fresh;                                           // last of its unit
-        if (lane == 0) q[0] = info0, q[1] = info1, q[2] = info2;
+        if (kTma) {
+            if (box_shift == 4) {
+                if (in_page >= p.batch.page) in_page = 0, ++slot;
+                if (in_page == 0 || fresh) page = slot < pages.n ? __ldg(pages.pages + slot) : -1;
+                a.page0 = page;
+                a.in_page = in_page;
+                in_page += kWarpTile;
+            } else {
+                const int slot0 = (int)p.by_page.of((unsigned)a.key0), slot1 = (int)p.by_page.of((unsigned)a.key0 + 8u);
+                a.in_page = a.key0 - slot0 * p.batch.page;
+                if (slot0 < pages.n) a.page0 = __ldg(pages.pages + slot0);
+                if (slot1 < pages.n && a.keys > 8) a.page1 = __ldg(pages.pages + slot1);
+            }
+        } else if (lane < a.keys) {
+            a.place = key_row(pages, p.batch, p.by_page, a.key0 + lane, p.kv_heads, w.h);
+        }
+        const bool inside = w.left > 1 && a.key0 + kWarpTile < w.hi;     // the unit goes on in this share
+        if (lane == 0) s_tiles[asked % S::kInfos] = make_int2(a.key0, (fresh ? 1 << 16 : 0) | (inside ? 0 : 1 << 17) | units << 18);
+        if (inside) {
+            --w.left;
+            ++w.tile;
+        } else {
+            more = w.next(p);
+        }
+        fresh = !inside;
         ++asked;
-        return found;
+        return a;
     };
-    auto view = [&](const int4* q, Walk& u) {                      // as row_place and row_limit need it
-        u.hi = q[0].y, u.b = q[1].x, u.rt = q[1].y, u.h = q[1].z, u.first = q[1].w, u.tokens = q[2].x, u.held = q[2].y;
+    auto view = [&](int at, Walk& u) {                             // a unit, as row_place and row_limit need it
+        const int4* const q = s_units + at % S::kInfos * 2;
+        const int4 x = q[0], y = q[1];
+        u.b = x.x, u.rt = x.y, u.h = x.z, u.first = x.w, u.tokens = y.x, u.held = y.y, u.hi = y.z, u.unit = y.w;
     };
-    auto fetch = [&](long long found) {
-        if (fetched < asked) {
-            int4* const q = s_info + fetched % S::kInfos * 3;
-            const int stage = fetched % S::kStages, keys = min(kWarpTile, q[0].y - q[0].x);
-            const uint32_t dst = ring0 + stage * 2 * S::kTileBytes;
-            unsigned there = __ballot_sync(0xFFFFFFFFu, found >= 0);   // keys that there are
+    auto fetch = [&](const Asked& a) {
+        if (a.real) {
+            const int stage = fetched % S::kStages;
+            const uint32_t dst = ring0 + stage * 2 * S::kTileBytes, full = bar + stage * 8;
+            unsigned there;                                        // keys that there are
             if (kTma) {
-                const int rows = 1 << box_shift;
-                if (lane == 0) mbar_expect_tx(bar + stage * 8, (uint32_t)__popc(there) * rows * DP * 4);
-                __syncwarp();
-                if (found >= 0) {
-                    const int key = q[0].x + lane * rows, in_page = key - (int)p.by_page.of((unsigned)key) * p.batch.page;
-                    const int plane = (int)found * p.kv_heads + q[1].z;
+                const bool ok0 = (unsigned)a.page0 < (unsigned)p.batch.n_pages, ok1 = (unsigned)a.page1 < (unsigned)p.batch.n_pages;
+                if (elect_one()) {
+                    const uint32_t box = DP * 4u << box_shift;     // bytes of a box of keys and one of values
+                    mbar_expect_tx(full, (ok0 ? box : 0u) + (ok1 ? box : 0u));
+                    if (ok0) {
+                        const int plane = a.page0 * p.kv_heads + a.h;
+                        if (box_shift == 4) {
+                            tma_load_4d(dst, &tmK, 0, a.in_page, 0, plane, full);
+                            tma_load_4d(dst + S::kTileBytes, &tmV, 0, a.in_page, 0, plane, full);
+                        } else {
 #pragma unroll
-                    for (int c = 0; c < DP / 64; ++c) {
-                        tma_load_3d(dst + c * (kWarpTile * 128) + lane * rows * 128, &tmK, c * 64, in_page, plane, bar + stage * 8);
-                        tma_load_3d(dst + S::kTileBytes + c * (kWarpTile * 128) + lane * rows * 128, &tmV, c * 64, in_page, plane, bar + stage * 8);
+                            for (int c = 0; c < DP / 64; ++c) {    // (a box of 8 keys fills half of a swizzled block: 64 entries at a time)
+                                tma_load_4d(dst + c * (kWarpTile * 128), &tmK, 0, a.in_page, c, plane, full);
+                                tma_load_4d(dst + S::kTileBytes + c * (kWarpTile * 128), &tmV, 0, a.in_page, c, plane, full);
+                            }
+                        }
+                    }
+                    if (ok1) {                                     // the tile's second half, in pages of 8, 24, ...
+                        const int key = a.key0 + 8, at = key - (int)p.by_page.of((unsigned)key) * p.batch.page, plane = a.page1 * p.kv_heads + a.h;
+#pragma unroll
+                        for (int c = 0; c < DP / 64; ++c) {
+                            tma_load_4d(dst + c * (kWarpTile * 128) + 1024, &tmK, 0, at, c, plane, full);
+                            tma_load_4d(dst + S::kTileBytes + c * (kWarpTile * 128) + 1024, &tmV, 0, at, c, plane, full);
+                        }
                     }
                 }
-                unsigned all = 0;
-                for (int i = 0; i < kWarpTile; i += rows)
-                    if (there >> (i >> box_shift) & 1u) all |= ((1u << rows) - 1u) << i;
-                there = all & (0xFFFFu >> (kWarpTile - keys));
+                __syncwarp();
+                there = ((ok0 ? box_shift == 4 ? 0xFFFFu : 0xFFu : 0u) | (ok1 ? 0xFF00u : 0u)) & (0xFFFFu >> (kWarpTile - a.keys));
             } else {
+                there = __ballot_sync(0xFFFFFFFFu, a.place >= 0);
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i) {
                     const int x = lane + 32 * i, r = x / S::kChunks, c = x % S::kChunks;
-                    const long long row = __shfl_sync(0xFFFFFFFFu, found, r);
+                    const long long row = __shfl_sync(0xFFFFFFFFu, a.place, r);
                     const bool real = row >= 0 && c * 8 < p.dim;
                     const size_t at = real ? (size_t)row * p.dim + c * 8 : 0;
                     cp_async16(dst + swz(r, c), (const __nv_bfloat16*)p.k + at, real);
                     cp_async16(dst + S::kTileBytes + swz(r, c), (const __nv_bfloat16*)p.v + at, real);
                 }
             }
-            if (lane == 0) q[0].z = (int)there;
-            if (q[2].z && lane < kWarpRows) {                      // a new unit: its queries towards L1
+            if (lane == 0) s_tiles[fetched % S::kInfos].y |= (int)there;
+            if (a.fresh && lane < kWarpRows) {                     // a new unit: its queries towards L1
                 Walk u;
-                view(q, u);
+                view(s_tiles[fetched % S::kInfos].y >> 18, u);
                 int t, g;
                 if (row_place(p, u, lane, t, g)) {
                     const char* src = (const char*)((const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(u.h * p.group + g) * p.q_h);
@@ -129,22 +177,22 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
         if (!kTma) cp_async_commit();
     };
-    long long pending;
+    Asked pending;
     {
-        long long found[S::kStages];
+        Asked first[S::kStages];
 #pragma unroll
-        for (int i = 0; i < S::kStages; ++i) found[i] = ask();     // (their page numbers are under way together)
+        for (int i = 0; i < S::kStages; ++i) first[i] = ask();     // (their page numbers are under way together)
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < S::kStages - 1; ++i) fetch(found[i]);
-        pending = found[S::kStages - 1];
+        for (int i = 0; i < S::kStages - 1; ++i) fetch(first[i]);
+        pending = first[S::kStages - 1];
     }
 
     const bool q_even = (((uintptr_t)p.q & 3) | ((uintptr_t)(p.q_t | p.q_h) & 1)) == 0;        // pairs of entries in one load
     const int row0 = lane >> 2, col = (lane & 3) * 2;              // this thread's rows of a unit: row0 and row0 + 8
     float o[DP / 8][4], m[2], l[2];
     uint32_t qf[DP / 16][4];
-    int lim[2], lim_all = 0, tokens = 0;
+    int lim[2], lim_all = 0, tokens = 0, unit = 0;
     bool ok = true;
     for (int tile = 0; tile < asked; ++tile) {
         const int stage = tile % S::kStages;
@@ -154,12 +202,12 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         __syncwarp();
         fetch(pending);
         pending = ask();
-        const int4* const q = s_info + tile % S::kInfos * 3;
-        const int4 at = q[0];                                      // first key, keys that the unit sees, keys that there are, unit
-        const bool last = q[2].w;
-        if (q[2].z) {                                              // a new unit
+        const int2 at = s_tiles[tile % S::kInfos];                 // first key; keys that there are, first and last of its unit, unit
+        const bool last = at.y >> 17 & 1;
+        if (at.y >> 16 & 1) {                                      // a new unit
             Walk u;
-            view(q, u);
+            view(at.y >> 18, u);
+            unit = u.unit;
             tokens = u.b < 0 ? 1 : u.tokens;
             int t, g;
             row_place(p, u, 0, t, g);
@@ -197,26 +245,24 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             mma_bf16(ks & 1 ? s2[0] : s[0], qf[ks], kf[0], kf[1]);
             mma_bf16(ks & 1 ? s2[1] : s[1], qf[ks], kf[2], kf[3]);
         }
-        // scores in units of log2; keys without a place or past a row's limit count as -inf
-        float top[2] = {m[0], m[1]};
-        const bool masked = at.x + kWarpTile > lim_all, some = masked || at.z != 0xFFFF;
+        // Keys without a place or past a row's limit count as -inf.  A row's reference m (in units of log2) stays until a
+        // score is 8 above it: weights stay below 2^8, and most tiles need neither the row's maximum nor a new scale of o.
+        const bool masked = at.x + kWarpTile > lim_all, some = masked || (at.y & 0xFFFF) != 0xFFFF;
+        float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int kk = i * 8 + col + (j & 1);
                 s[i][j] = (s[i][j] + s2[i][j]) * p.scale_log2;
-                if (some && (!(at.z >> kk & 1) || at.x + kk >= lim[j >> 1])) s[i][j] = -INFINITY;
+                if (some && (!(at.y >> kk & 1) || at.x + kk >= lim[j >> 1])) s[i][j] = -INFINITY;
                 top[j >> 1] = fmaxf(top[j >> 1], s[i][j]);
             }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 1));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 2));
-        }
-        if (__any_sync(0xFFFFFFFFu, top[0] > m[0] || top[1] > m[1])) {
+        if (__any_sync(0xFFFFFFFFu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f)) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 1));
+                top[i] = fmaxf(m[i], fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 2)));
                 const float f = m[i] == -INFINITY ? 0.f : exp2_fast(m[i] - top[i]);
                 m[i] = top[i];
                 l[i] *= f;
@@ -238,10 +284,10 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             l[0] += s[i][0] + s[i][1];
             l[1] += s[i][2] + s[i][3];
         }
-        if (kTma && at.z != 0xFFFF) {                              // what lies in the place of keys that there are not
+        if (kTma && (at.y & 0xFFFF) != 0xFFFF) {                              // what lies in the place of keys that there are not
 #pragma unroll
             for (int r = 0; r < kWarpTile; ++r)
-                if (!(at.z >> r & 1) && lane < S::kChunks) *reinterpret_cast<uint4*>(ring + (vt - ring0) + swz(r, lane)) = make_uint4(0u, 0u, 0u, 0u);
+                if (!(at.y >> r & 1) && lane < S::kChunks) *reinterpret_cast<uint4*>(ring + (vt - ring0) + swz(r, lane)) = make_uint4(0u, 0u, 0u, 0u);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         }
@@ -284,8 +330,8 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 mma_bf16(o[2 * d + 1], pf, vf[2], vf[3]);
             }
         }
-        if (last && at.w + worker < p.here.pieces) {
-            const size_t piece = (size_t)(at.w + worker) * kWarpRows;
+        if (last && unit + worker < p.here.pieces) {
+            const size_t piece = (size_t)(unit + worker) * kWarpRows;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 1);

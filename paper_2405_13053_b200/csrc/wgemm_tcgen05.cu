@@ -167,6 +167,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
         ::"r"(dst), "l"((uint64_t)tm), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"((uint64_t)tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+}
 // Shared memory -> global tensor tile; the calling thread waits until the copy has completed.
 __device__ __forceinline__ void tma_store_2d_and_wait(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
@@ -3062,21 +3068,22 @@ bool prefix_tc_supported(const AttendSizes& z) {
            rows < (1LL << 31) - kPfxRows && z.n_pages > 0 && z.n_pages * z.kv_heads < (1LL << 31);
 }
 
-// Tensor map of a cache [pages * kv_heads][page_size][D]: boxes of 64 entries x `rows` keys, 128-byte swizzled.
-static int get_cache_map(const void* ptr, int D, int page_size, long long planes, int rows, CUtensorMap* out) {
+// Tensor map of a cache [pages * kv_heads][page_size][D] as (64 entries, keys, blocks of 64 entries, planes): a box is `rows` keys and
+// `blocks` blocks, each block's keys one after the other in shared memory, 128-byte swizzled.
+static int get_cache_map(const void* ptr, int D, int page_size, long long planes, int rows, int blocks, CUtensorMap* out) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return METEORA_ERR_CUDA;
-    const cuuint64_t gdim[3] = {(cuuint64_t)D, (cuuint64_t)page_size, (cuuint64_t)planes};
-    const cuuint64_t gstride[2] = {(cuuint64_t)D * 2, (cuuint64_t)D * 2 * page_size};
-    const cuuint32_t box[3] = {64, (cuuint32_t)rows, 1}, estride[3] = {1, 1, 1};
-    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const cuuint64_t gdim[4] = {64, (cuuint64_t)page_size, (cuuint64_t)D / 64, (cuuint64_t)planes};
+    const cuuint64_t gstride[3] = {(cuuint64_t)D * 2, 128, (cuuint64_t)D * 2 * page_size};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, (cuuint32_t)blocks, 1}, estride[4] = {1, 1, 1, 1};
+    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? METEORA_OK : METEORA_ERR_CUDA;
 }
 
 template <int D>
 static int launch_prefix_tc_d(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixTcParams& pp, cudaStream_t st) {
-    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.prefix.workers), kThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
+    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.prefix.workers), kPfxThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
 }
 
 int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
@@ -3088,8 +3095,8 @@ int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
     pp.a.scale_log2 = pp.sign ? fabsf(p.scale_log2) : 1.f;
     CUtensorMap tk, tv;
     int rc;
-    if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tk)) != METEORA_OK) return rc;
-    if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, &tv)) != METEORA_OK) return rc;
+    if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, 1, &tk)) != METEORA_OK) return rc;
+    if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, 1, &tv)) != METEORA_OK) return rc;
     return p.dim == 64 ? launch_prefix_tc_d<64>(tk, tv, pp, st) : launch_prefix_tc_d<128>(tk, tv, pp, st);
 }
 
@@ -3098,8 +3105,9 @@ static int launch_attend_warp_d(const AttendParams& p, int box_rows, cudaStream_
     CUtensorMap tk = {}, tv = {};
     int rc, shift = 0;
     if (kTma) {
-        if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, &tk)) != METEORA_OK) return rc;
-        if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, &tv)) != METEORA_OK) return rc;
+        const int blocks = box_rows == kWarpTile ? DP / 64 : 1;
+        if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, blocks, &tk)) != METEORA_OK) return rc;
+        if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, blocks, &tv)) != METEORA_OK) return rc;
         while ((1 << shift) < box_rows) ++shift;
     }
     return launch_dependent<k_attend_warp<DP, kTma>>(dim3(p.here.workers / 4), 128, AttendWarpShape<DP>::kBytes, st, tk, tv, p, shift);
