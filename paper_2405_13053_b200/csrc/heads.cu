@@ -1,11 +1,13 @@
 // Rotary positions, norms of query and key heads, and the append to a paged cache: one pass over rows of heads.
 //
 // A row is one head of one token.  A group of lanes holds it in registers as items of two vectors (heads.cuh): the two
-// entries of a pair are in one thread, the norm's sum is a few shuffles.  A CTA takes a token (its rows, or a share
-// of them where there are few tokens), so that the cos and sin of the token's pairs are computed once, by rot/2 threads, and
-// read from shared memory by all its heads: sincospif for every row would take as long as the row's bytes.
+// entries of a pair are in one thread, the norm's sum is a few shuffles.  A CTA takes a few tokens: their places and the cos
+// and sin of their pairs are worked out once, by all its threads, and read from shared memory by all their heads
+// (sincospif for every row would take as long as the row's bytes); then its groups walk the tokens' rows, kAhead at a time,
+// the first of which are asked for before the angles.  Few tokens: one per CTA, its rows dealt over several CTAs.
 // Bound by HBM: every entry is read once and written once.
 #include <algorithm>
+#include <stdlib.h>
 
 #include "heads.cuh"
 #include "launch_heads.cuh"
@@ -23,9 +25,12 @@ struct HeadSeg {
     int heads, paged, turn;
 };
 
+constexpr int kMaxTokens = 8;      // of a CTA at a time
+constexpr int kAhead = 2;          // rows of a group under way
+
 struct HeadPassParams {
     HeadSeg seg[3];
-    int rows, rows_per_cta, groups, lanes, items;
+    int rows, rows_per_cta, tokens, groups, lanes, lane_shift, items;
     int T, dim, p64, batched, inverse;
     const void* positions;
     float eps;
@@ -33,131 +38,159 @@ struct HeadPassParams {
     meteora_rotary_t rot;    // dim 0: no rotation
 };
 
-template <typename E, int VE, int NI>
-__global__ void __launch_bounds__(kHeadThreads) k_head_pass(const __grid_constant__ HeadPassParams p) {
+template <typename E, int VE, int NI, bool kNorm>
+__global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(const __grid_constant__ HeadPassParams p) {
     typedef HeadVec<E, VE> V;
-    __shared__ float2 s_cs[kMaxPairs];
-    __shared__ int s_at[2];
-    __shared__ long long s_pos;
-    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid / p.lanes;
-    const int t = blockIdx.x;
-    const int row_lo = blockIdx.y * p.rows_per_cta, row_hi = min(p.rows, row_lo + p.rows_per_cta);
+    extern __shared__ __align__(16) uint8_t s_rows[];           // [kAhead][2 NI][threads] vectors
+    __shared__ float2 s_cs[kMaxTokens][kMaxPairs];
+    __shared__ int s_page[kMaxTokens], s_in_page[kMaxTokens];
+    __shared__ long long s_pos[kMaxTokens];
+    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid >> p.lane_shift;
+    const int t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
+    const int row_lo = blockIdx.y * p.rows_per_cta, rows = min(p.rows, row_lo + p.rows_per_cta) - row_lo;    // of each token
     const HeadItems it(p.dim, p.rot.dim, p.rot.layout == METEORA_ROTARY_HALF, VE);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    typename V::Raw a[NI], b[NI];
-    auto seg_of = [&](int r, int& h) {
-        int s = 0;
-        h = r;
-        if (h >= p.seg[0].heads) h -= p.seg[0].heads, s = 1;
-        if (s == 1 && h >= p.seg[1].heads) h -= p.seg[1].heads, s = 2;
-        return s;
-    };
-    auto load_row = [&](int r) {
-        if (r >= row_hi) return;
-        int h;
-        const HeadSeg& g = p.seg[seg_of(r, h)];
-        const E* src = (const E*)g.in + t * g.in_t + h * g.in_h;
+    int oa[NI], ob[NI];                         // where this thread's items start; no second vector: ob >= dim
 #pragma unroll
-        for (int n = 0; n < NI; ++n) {
-            const int i = lane + n * p.lanes;
-            a[n] = b[n] = V::zero();
-            if (i < p.items) {
-                a[n] = V::load(src + it.a(i, VE));
-                if (it.b(i, VE) < p.dim) b[n] = V::load(src + it.b(i, VE));
-            }
-        }
+    for (int n = 0; n < NI; ++n) {
+        const int i = lane + n * p.lanes;
+        oa[n] = i < p.items ? it.a(i, VE) : p.dim;
+        ob[n] = i < p.items ? it.b(i, VE) : p.dim;
+    }
+    typedef typename V::Raw Raw;
+    const auto place = [&](int slot, int v) { return reinterpret_cast<Raw*>(s_rows) + (slot * 2 * NI + v) * blockDim.x + tid; };
+    const auto seg_of = [&](int r, int& h) {
+        h = row_lo + r;
+        if (h < p.seg[0].heads) return 0;
+        h -= p.seg[0].heads;
+        if (h < p.seg[1].heads) return 1;
+        h -= p.seg[1].heads;
+        return 2;
     };
-    load_row(row_lo + group);                   // on its way while the token's place and angles are worked out
+    // a group's rows: token tt of the CTA's, row rr of the token's; `far` runs kAhead rows ahead
+    const auto step = [&](int& tt, int& rr) {
+        rr += p.groups;
+        while (rr >= rows) rr -= rows, ++tt;
+    };
+    int far_t = 0, far_r = group, asked = 0;
+    while (far_r >= rows) far_r -= rows, ++far_t;
+    if (group >= p.groups) far_t = nt;          // (lanes that fill the last warp)
+    int tt = far_t, rr = far_r;
+    const auto ask = [&]() {
+        if (far_t < nt) {
+            int h;
+            const HeadSeg& g = p.seg[seg_of(far_r, h)];
+            const E* src = (const E*)g.in + (t0 + far_t) * g.in_t + h * g.in_h;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) {
+                if (oa[n] < p.dim) row_copy(place(asked % kAhead, 2 * n), src + oa[n]);
+                if (ob[n] < p.dim) row_copy(place(asked % kAhead, 2 * n + 1), src + ob[n]);
+            }
+            step(far_t, far_r);
+        }
+        ++asked;
+        row_commit();
+    };
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) ask();
 
     if (p.batched) {
-        if (tid < 32) {
-            const int seq = sequence_of(p.batch, t, tid);
-            if (tid == 0) {
-                int held = seq >= 0 ? __ldg(p.batch.lengths + seq) : -1;
+        for (int k = tid >> 5; k < nt; k += blockDim.x >> 5) {
+            const int t = t0 + k, seq = sequence_of(p.batch, t, tid & 31);
+            if ((tid & 31) == 0) {
+                const int held = seq >= 0 ? __ldg(p.batch.lengths + seq) : -1;
                 long long i = -1, page = -1;
                 if (held >= 0) {
                     i = (long long)held + (p.batch.cu ? t - __ldg(p.batch.cu + seq) : 0);
                     const long long slot = i / p.batch.page;
                     if (slot < p.batch.width) page = __ldg(p.batch.table + (size_t)seq * p.batch.width + slot);
-                    if (page >= p.batch.n_pages) page = -1;
+                    if (page >= p.batch.n_pages || page < 0) page = -1;
                 }
-                s_pos = p.batch.prefix + i;
-                s_at[0] = held >= 0 ? (int)page : -2;
-                s_at[1] = held >= 0 ? (int)(i % p.batch.page) : 0;
+                s_pos[k] = p.batch.prefix + i;
+                s_page[k] = held >= 0 ? (int)page : -2;
+                s_in_page[k] = held >= 0 ? (int)(i % p.batch.page) : 0;
             }
         }
         __syncthreads();
-        if (s_at[0] == -2) return;              // no sequence: nothing of this token is written
     }
-    if (p.rot.dim > 0) {
-        const long long pos = p.batched ? s_pos
-                              : p.p64   ? __ldg((const long long*)p.positions + t)
-                                        : (long long)__ldg((const int32_t*)p.positions + t);
-        for (int i = tid; i < p.rot.dim / 2; i += blockDim.x)
-            s_cs[i] = rotary_pair(p.rot.turns[i], pos, p.inverse != 0, p.rot.scale);
+    const int pairs = p.rot.dim / 2;
+    if (pairs > 0) {
+        for (int i = tid, k = 0; i < nt * pairs; i += blockDim.x) {
+            k = i / pairs;
+            const long long pos = p.batched ? s_pos[k]
+                                  : p.p64   ? __ldg((const long long*)p.positions + t0 + k)
+                                            : (long long)__ldg((const int32_t*)p.positions + t0 + k);
+            const int q = i - k * pairs;
+            s_cs[k][it.table(q, VE)] = rotary_pair(p.rot.turns[q], pos, p.inverse != 0, p.rot.scale);
+        }
         __syncthreads();
     }
-    const bool has_place = !p.batched || s_at[0] >= 0;
     // (whole warps stay in the loop: the norm's shuffles need every lane)
-    for (int r0 = row_lo; r0 < row_hi; r0 += p.groups) {
-        const int r = r0 + group;
-        const bool live = r < row_hi && group < p.groups;
+    int used = 0;
+    for (int done = 0; done < nt * rows; done += p.groups, ++used) {
+        row_wait<kAhead - 1>();
+        const bool live = tt < nt;
         int h = 0;
-        const HeadSeg& g = p.seg[live ? seg_of(r, h) : 0];
-        typename V::Raw ya[NI], yb[NI];
-        float sum = 0.f;
+        const HeadSeg& g = p.seg[live ? seg_of(rr, h) : 0];
+        Raw a[NI], b[NI];
         float xa[NI][VE], xb[NI][VE];
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
-            ya[n] = a[n];
-            yb[n] = b[n];
+            a[n] = live && oa[n] < p.dim ? *place(used % kAhead, 2 * n) : V::zero();
+            b[n] = live && ob[n] < p.dim ? *place(used % kAhead, 2 * n + 1) : V::zero();
             V::unpack(a[n], xa[n]);
             V::unpack(b[n], xb[n]);
-#pragma unroll
-            for (int j = 0; j < VE; ++j) sum = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], sum));
         }
-        load_row(r + p.groups);
-        const bool norm = live && g.gain != nullptr;
-        if (p.seg[0].gain || p.seg[1].gain) sum = lanes_sum(sum, p.lanes);
-        const float rs = norm ? 1.f / sqrtf(sum / (float)p.dim + p.eps) : 1.f;
-        if (!live || (g.paged && !has_place)) continue;
-        E* dst = g.paged ? (E*)g.out + (((int64_t)s_at[0] * g.heads + h) * p.batch.page + s_at[1]) * p.dim
-                         : (E*)g.out + t * g.out_t + h * g.out_h;
+        ask();
+        if (kNorm) {
+            float sum = 0.f, none = 0.f;
 #pragma unroll
-        for (int n = 0; n < NI; ++n) {
-            const int i = lane + n * p.lanes;
-            if (i >= p.items) continue;
-            const int oa = it.a(i, VE), ob = it.b(i, VE);
-            if (norm) {
-                float ga[VE], gb[VE];
-                V::unpack(V::load((const E*)g.gain + oa), ga);
-                V::unpack(ob < p.dim ? V::load((const E*)g.gain + ob) : V::zero(), gb);
+            for (int n = 0; n < NI; ++n)
 #pragma unroll
-                for (int j = 0; j < VE; ++j) xa[n][j] *= rs * ga[j], xb[n][j] *= rs * gb[j];
-            }
-            if (g.turn && i < it.nr) {
-                float2 cs[VE];
+                for (int j = 0; j < VE; ++j) sum = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], sum));
+            lanes_sum(sum, none, p.lanes);
+            if (g.gain) {
+                const float rs = 1.f / sqrtf(sum / (float)p.dim + p.eps);
 #pragma unroll
-                for (int j = 0; j < VE; ++j) cs[j] = s_cs[i * VE + j];
-                turn_item<VE>(xa[n], xb[n], cs, it.half);
+                for (int n = 0; n < NI; ++n) {
+                    float ga[VE], gb[VE];
+                    V::unpack(oa[n] < p.dim ? V::load((const E*)g.gain + oa[n]) : V::zero(), ga);
+                    V::unpack(ob[n] < p.dim ? V::load((const E*)g.gain + ob[n]) : V::zero(), gb);
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) xa[n][j] *= rs * ga[j], xb[n][j] *= rs * gb[j];
+                }
             }
-            if (norm || (g.turn && i < it.nr)) {
-                ya[n] = V::pack(xa[n]);
-                yb[n] = V::pack(xb[n]);
-            }
-            V::store(dst + oa, ya[n]);
-            if (ob < p.dim) V::store(dst + ob, yb[n]);
         }
+        const int page = !p.batched || !live ? 0 : s_page[tt];           // -2: no sequence, -1: no page
+        if (live && page > -2 && (page >= 0 || !g.paged)) {
+            E* const dst = g.paged ? (E*)g.out + (((int64_t)page * g.heads + h) * p.batch.page + s_in_page[tt]) * p.dim
+                                   : (E*)g.out + (t0 + tt) * g.out_t + h * g.out_h;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) {
+                if (oa[n] >= p.dim) continue;
+                const int i = lane + n * p.lanes;
+                const bool turn = g.turn && i < it.nr;
+                if (turn) {
+                    float2 cs[VE];
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) cs[j] = s_cs[tt][j * it.nr + i];
+                    turn_item<VE>(xa[n], xb[n], cs, it.half);
+                }
+                const bool same = !turn && !(kNorm && g.gain);           // bit for bit
+                V::store(dst + oa[n], same ? a[n] : V::pack(xa[n]));
+                if (ob[n] < p.dim) V::store(dst + ob[n], same ? b[n] : V::pack(xb[n]));
+            }
+        }
+        if (live) step(tt, rr);
     }
 }
 
 // Gradients of the norm with the rotation.  CTAs [0, q_ctas) take q, the others k; a CTA walks its share of the tokens,
-// kTokTile at a time (their angles by all its threads at once), and keeps its rows' sum of dn * n in registers: one row
-// of partial sums per CTA goes to the workspace, and k_gain_sums adds those up in their order.
-constexpr int kTokTile = 4;
-
+// kMaxTokens at a time (their angles by all its threads at once), and keeps its rows' sum of dn * n in registers: one row
+// of partial sums per CTA goes to the workspace, and k_gain_sums adds those up in their order.  Bound by HBM: x and dy
+// are read once, dx written once.
 struct HeadGradSeg {
     const void* dy;
     const void* x;
@@ -168,7 +201,7 @@ struct HeadGradSeg {
 };
 struct HeadGradParams {
     HeadGradSeg seg[2];
-    int q_ctas, groups, lanes, items;
+    int q_ctas, groups, lanes, lane_shift, items;
     int T, dim, p64;
     const void* positions;
     float eps;
@@ -177,119 +210,160 @@ struct HeadGradParams {
 };
 
 template <typename E, int VE, int NI>
-__global__ void __launch_bounds__(kHeadThreads) k_head_grad(const __grid_constant__ HeadGradParams p) {
+__global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_constant__ HeadGradParams p) {
     typedef HeadVec<E, VE> V;
-    __shared__ float2 s_cs[kTokTile][kMaxPairs];
-    __shared__ float s_sum[METEORA_MAX_HEAD_DIM];
-    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid / p.lanes;
+    __shared__ float2 s_cs[kMaxTokens][kMaxPairs];
+    __shared__ float s_sum[8][METEORA_MAX_HEAD_DIM];
+    extern __shared__ __align__(16) uint8_t s_rows[];           // [kAhead][4 NI][threads] vectors
+    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid >> p.lane_shift;
     const bool is_k = (int)blockIdx.x >= p.q_ctas;
     const HeadGradSeg& g = p.seg[is_k ? 1 : 0];
     const int ctas = is_k ? gridDim.x - p.q_ctas : p.q_ctas, cta = is_k ? blockIdx.x - p.q_ctas : blockIdx.x;
     const int t_lo = (int)((long long)p.T * cta / ctas), t_hi = (int)((long long)p.T * (cta + 1) / ctas);
     const HeadItems it(p.dim, p.rot.dim, p.rot.layout == METEORA_ROTARY_HALF, VE);
-    const int pairs = p.rot.dim / 2;
+    const int pairs = p.rot.dim / 2, heads = g.heads;
+    const float inv_dim = 1.f / (float)p.dim;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float ga[NI][VE], gb[NI][VE], da[NI][VE], db[NI][VE];
+    int oa[NI], ob[NI];
+    typename V::Raw gain_a[NI], gain_b[NI];
+    float da[NI][VE], db[NI][VE];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
         const int i = lane + n * p.lanes;
-        V::unpack(i < p.items ? V::load((const E*)g.gain + it.a(i, VE)) : V::zero(), ga[n]);
-        V::unpack(i < p.items && it.b(i, VE) < p.dim ? V::load((const E*)g.gain + it.b(i, VE)) : V::zero(), gb[n]);
+        oa[n] = i < p.items ? it.a(i, VE) : p.dim;
+        ob[n] = i < p.items ? it.b(i, VE) : p.dim;
+        gain_a[n] = oa[n] < p.dim ? V::load((const E*)g.gain + oa[n]) : V::zero();
+        gain_b[n] = ob[n] < p.dim ? V::load((const E*)g.gain + ob[n]) : V::zero();
 #pragma unroll
         for (int j = 0; j < VE; ++j) da[n][j] = db[n][j] = 0.f;
     }
-    for (int t0 = t_lo; t0 < t_hi; t0 += kTokTile) {
-        const int nt = min(kTokTile, t_hi - t0);
-        __syncthreads();
-        for (int i = tid; i < nt * pairs; i += blockDim.x) {
-            const int tt = i / pairs, q = i - tt * pairs;
-            const long long pos = p.p64 ? __ldg((const long long*)p.positions + t0 + tt)
-                                        : (long long)__ldg((const int32_t*)p.positions + t0 + tt);
-            s_cs[tt][q] = rotary_pair(p.rot.turns[q], pos, true, p.rot.scale);
-        }
-        __syncthreads();
-        const int rows = nt * g.heads;
-        for (int r0 = 0; r0 < rows; r0 += p.groups) {
-            const int r = r0 + group;
-            const bool live = r < rows && group < p.groups;
-            const int tt = live ? r / g.heads : 0, h = live ? r - tt * g.heads : 0;
-            const int64_t t = t0 + tt;
-            const E* x = (const E*)g.x + t * g.x_t + h * g.x_h;
-            const E* dy = (const E*)g.dy + t * g.dy_t + h * g.dy_h;
-            float xa[NI][VE], xb[NI][VE], ya[NI][VE], yb[NI][VE];
-            typename V::Raw ra[NI], rb[NI], sa[NI], sb[NI];
+    const auto step = [&](int& t, int& h) {
+        h += p.groups;
+        while (h >= heads) h -= heads, ++t;
+    };
+    typedef typename V::Raw Raw;
+    const auto place = [&](int slot, int v) { return reinterpret_cast<Raw*>(s_rows) + (slot * 4 * NI + v) * kHeadThreads + tid; };
+    // a group's rows: token t, head h; `far` runs kAhead rows ahead
+    int next_t = t_lo, next_h = group, asked = 0, used = 0;
+    while (next_h >= heads) next_h -= heads, ++next_t;
+    int far_t = next_t, far_h = next_h;
+    const auto ask = [&]() {
+        if (far_t < t_hi) {
+            const E* x = (const E*)g.x + far_t * g.x_t + far_h * g.x_h;
+            const E* dy = (const E*)g.dy + far_t * g.dy_t + far_h * g.dy_h;
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
-                const int i = lane + n * p.lanes;
-                const bool in = live && i < p.items, in_b = in && it.b(i, VE) < p.dim;
-                ra[n] = in ? V::load(x + it.a(i, VE)) : V::zero();
-                sa[n] = in ? V::load(dy + it.a(i, VE)) : V::zero();
-                rb[n] = in_b ? V::load(x + it.b(i, VE)) : V::zero();
-                sb[n] = in_b ? V::load(dy + it.b(i, VE)) : V::zero();
+                if (oa[n] < p.dim) {
+                    row_copy(place(asked % kAhead, 4 * n), x + oa[n]);
+                    row_copy(place(asked % kAhead, 4 * n + 1), dy + oa[n]);
+                }
+                if (ob[n] < p.dim) {
+                    row_copy(place(asked % kAhead, 4 * n + 2), x + ob[n]);
+                    row_copy(place(asked % kAhead, 4 * n + 3), dy + ob[n]);
+                }
             }
+            step(far_t, far_h);
+        }
+        ++asked;
+        row_commit();
+    };
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) ask();
+    for (int t0 = t_lo; t0 < t_hi; t0 += kMaxTokens) {
+        const int nt = min(kMaxTokens, t_hi - t0);
+        if (pairs > 0) {
+            __syncthreads();
+            for (int i = tid; i < nt * pairs; i += blockDim.x) {
+                const int k = i / pairs, q = i - k * pairs;
+                const long long pos = p.p64 ? __ldg((const long long*)p.positions + t0 + k)
+                                            : (long long)__ldg((const int32_t*)p.positions + t0 + k);
+                s_cs[k][it.table(q, VE)] = rotary_pair(p.rot.turns[q], pos, true, p.rot.scale);
+            }
+            __syncthreads();
+        }
+        // (every group has a row in each round, or none: whole warps stay in the loop)
+        while (__any_sync(0xFFFFFFFFu, next_t < t0 + nt)) {
+            const bool live = next_t < t0 + nt;
+            const int t = next_t, h = next_h;
+            float xa[NI][VE], xb[NI][VE], ya[NI][VE], yb[NI][VE];
             float sq = 0.f, dot = 0.f;
+            row_wait<kAhead - 1>();
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
                 const int i = lane + n * p.lanes;
-                V::unpack(ra[n], xa[n]);
-                V::unpack(rb[n], xb[n]);
-                V::unpack(sa[n], ya[n]);
-                V::unpack(sb[n], yb[n]);
-                if (i < it.nr) {
+                const bool in = live && oa[n] < p.dim, in_b = live && ob[n] < p.dim;
+                V::unpack(in ? *place(used % kAhead, 4 * n) : V::zero(), xa[n]);
+                V::unpack(in ? *place(used % kAhead, 4 * n + 1) : V::zero(), ya[n]);
+                V::unpack(in_b ? *place(used % kAhead, 4 * n + 2) : V::zero(), xb[n]);
+                V::unpack(in_b ? *place(used % kAhead, 4 * n + 3) : V::zero(), yb[n]);
+                if (i < it.nr && live) {
                     float2 cs[VE];
 #pragma unroll
-                    for (int j = 0; j < VE; ++j) cs[j] = s_cs[tt][i * VE + j];
+                    for (int j = 0; j < VE; ++j) cs[j] = s_cs[t - t0][j * it.nr + i];
                     turn_item<VE>(ya[n], yb[n], cs, it.half);
                 }
+                float ga[VE], gb[VE];
+                V::unpack(gain_a[n], ga);
+                V::unpack(gain_b[n], gb);
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
                     sq = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], sq));
-                    dot = fmaf(ga[n][j] * ya[n][j], xa[n][j], fmaf(gb[n][j] * yb[n][j], xb[n][j], dot));
+                    dot = fmaf(ga[j] * ya[n][j], xa[n][j], fmaf(gb[j] * yb[n][j], xb[n][j], dot));
                 }
             }
-            sq = lanes_sum(sq, p.lanes);
-            dot = lanes_sum(dot, p.lanes);
+            if (live) {
+                step(next_t, next_h);
+                ++used;
+                ask();
+            }
+            lanes_sum(sq, dot, p.lanes);
             if (!live) continue;
-            const float rs = 1.f / sqrtf(sq / (float)p.dim + p.eps);
-            const float mean = dot * rs / (float)p.dim;             // mean of gain * dn * n
+            const float rs = 1.f / sqrtf(sq * inv_dim + p.eps);
+            const float mean = dot * rs * inv_dim;                  // mean of gain * dn * n
             E* dx = (E*)g.dx + t * g.dx_t + h * g.dx_h;
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
-                const int i = lane + n * p.lanes;
-                if (i >= p.items) continue;
-                float oa[VE], ob[VE];
+                float ga[VE], gb[VE];
+                V::unpack(gain_a[n], ga);
+                V::unpack(gain_b[n], gb);
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
                     const float na = xa[n][j] * rs, nb = xb[n][j] * rs;
                     da[n][j] = fmaf(ya[n][j], na, da[n][j]);
                     db[n][j] = fmaf(yb[n][j], nb, db[n][j]);
-                    oa[j] = rs * (ga[n][j] * ya[n][j] - na * mean);
-                    ob[j] = rs * (gb[n][j] * yb[n][j] - nb * mean);
+                    xa[n][j] = rs * fmaf(ga[j], ya[n][j], -na * mean);
+                    xb[n][j] = rs * fmaf(gb[j], yb[n][j], -nb * mean);
                 }
-                V::store(dx + it.a(i, VE), V::pack(oa));
-                if (it.b(i, VE) < p.dim) V::store(dx + it.b(i, VE), V::pack(ob));
+                if (oa[n] < p.dim) V::store(dx + oa[n], V::pack(xa[n]));
+                if (ob[n] < p.dim) V::store(dx + ob[n], V::pack(xb[n]));
             }
         }
     }
-    // the groups' sums, group by group in order
-    for (int s = 0; s < p.groups; ++s) {
-        if (group == s) {
+    // the groups' sums: inside a warp by shuffles, then warp by warp in order
 #pragma unroll
-            for (int n = 0; n < NI; ++n) {
-                const int i = lane + n * p.lanes;
-                if (i >= p.items) continue;
+    for (int n = 0; n < NI; ++n)
 #pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    const int oa = it.a(i, VE) + j, ob = it.b(i, VE) + j;
-                    s_sum[oa] = s ? s_sum[oa] + da[n][j] : da[n][j];
-                    if (ob < p.dim) s_sum[ob] = s ? s_sum[ob] + db[n][j] : db[n][j];
-                }
+        for (int j = 0; j < VE; ++j)
+            for (int o = p.lanes; o < 32; o <<= 1) {
+                da[n][j] += __shfl_xor_sync(0xFFFFFFFFu, da[n][j], o);
+                db[n][j] += __shfl_xor_sync(0xFFFFFFFFu, db[n][j], o);
             }
-        }
-        __syncthreads();
+    if ((tid & 31) < p.lanes) {
+#pragma unroll
+        for (int n = 0; n < NI; ++n)
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                if (oa[n] < p.dim) s_sum[tid >> 5][oa[n] + j] = da[n][j];
+                if (ob[n] < p.dim) s_sum[tid >> 5][ob[n] + j] = db[n][j];
+            }
     }
-    for (int d = tid; d < p.dim; d += blockDim.x) p.part[(size_t)blockIdx.x * p.dim + d] = s_sum[d];
+    __syncthreads();
+    for (int d = tid; d < p.dim; d += blockDim.x) {
+        float v = s_sum[0][d];
+        for (int w = 1; w < (int)blockDim.x / 32; ++w) v += s_sum[w][d];
+        p.part[(size_t)blockIdx.x * p.dim + d] = v;
+    }
 }
 
 // Column sums of the partial rows: 32 columns per CTA, 32 threads per column, then a tree.  CTAs [0, col_ctas) for q.
@@ -340,6 +414,15 @@ static int vector_entries(meteora_dtype_t dtype, int dim, int rot, F all_aligned
 
 static int items_of(int dim, int rot, int ve) { return rot / 2 / ve + ((dim - rot) / ve + 1) / 2; }
 
+template <typename E, bool kNorm>
+static int launch_pass(int ve, dim3 grid, int threads, const HeadPassParams& p, cudaStream_t st) {
+    const size_t smem = (size_t)kAhead * 2 * (ve == 1 ? 4 : 1) * threads * ve * sizeof(E);
+    if (ve == 16 / (int)sizeof(E)) return launch_dependent<k_head_pass<E, 16 / (int)sizeof(E), 1, kNorm>>(grid, threads, smem, st, p);
+    if constexpr (sizeof(E) == 2)
+        if (ve == 4) return launch_dependent<k_head_pass<E, 4, 1, kNorm>>(grid, threads, smem, st, p);
+    return launch_dependent<k_head_pass<E, 1, 4, kNorm>>(grid, threads, smem, st, p);
+}
+
 int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args, cudaStream_t st) {
     if (args.T == 0) return METEORA_OK;
     HeadPassParams p = {};
@@ -372,32 +455,28 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     });
     p.items = items_of(p.dim, p.rot.dim, ve);
     p.lanes = std::min(32, pow2_at_least(p.items));
-    // A token's rows in as few rounds of 256 threads as they take, evenly; where there are fewer tokens than the device
-    // holds CTAs the rows are dealt over several CTAs.
-    int rounds = (p.rows * p.lanes + kHeadThreads - 1) / kHeadThreads;
-    int split = 1;
-    while (split < rounds && (long long)args.T * (split + 1) <= 592) ++split;
+    while ((1 << p.lane_shift) < p.lanes) ++p.lane_shift;
+    // Up to four tokens per CTA; few tokens: the rows of each dealt over several CTAs.
+    constexpr int kWave = 148 * 4;
+    p.tokens = getenv("TOK") ? atoi(getenv("TOK")) : std::min(4, (args.T + kWave - 1) / kWave);
+    int rounds = (p.rows * p.lanes + kHeadThreads - 1) / kHeadThreads, split = 1;
+    while (split < rounds && (long long)args.T * (split + 1) <= kWave) ++split;
     p.rows_per_cta = (p.rows + split - 1) / split;
     split = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
-    rounds = (p.rows_per_cta * p.lanes + kHeadThreads - 1) / kHeadThreads;
-    p.groups = (p.rows_per_cta + rounds - 1) / rounds;
+    p.groups = std::min(kHeadThreads / p.lanes, p.rows_per_cta * p.tokens);
     const int threads = (p.groups * p.lanes + 31) / 32 * 32;
-    const dim3 grid(args.T, split);
-    if (args.dtype == METEORA_BF16) {
-        if (ve == 8) return launch_dependent<k_head_pass<__nv_bfloat16, 8, 1>>(grid, threads, 0, st, p);
-        if (ve == 4) return launch_dependent<k_head_pass<__nv_bfloat16, 4, 1>>(grid, threads, 0, st, p);
-        return launch_dependent<k_head_pass<__nv_bfloat16, 1, 4>>(grid, threads, 0, st, p);
-    }
-    if (ve == 4) return launch_dependent<k_head_pass<float, 4, 1>>(grid, threads, 0, st, p);
-    return launch_dependent<k_head_pass<float, 1, 4>>(grid, threads, 0, st, p);
+    const dim3 grid((args.T + p.tokens - 1) / p.tokens, split);
+    bool norm = false;
+    for (int i = 0; i < n_segs; ++i) norm |= segs[i].gain != nullptr;
+    if (args.dtype == METEORA_BF16) return norm ? launch_pass<__nv_bfloat16, true>(ve, grid, threads, p, st) : launch_pass<__nv_bfloat16, false>(ve, grid, threads, p, st);
+    return norm ? launch_pass<float, true>(ve, grid, threads, p, st) : launch_pass<float, false>(ve, grid, threads, p, st);
 }
 
-// CTAs of the gradient kernel: a few per SM, each with at least a tile of tokens; q and k get shares as their heads are.
+// CTAs of the gradient kernel: two per SM (by registers), each with at least a few tokens; q and k get shares as their heads are.
 static void grad_ctas(int T, int q_heads, int k_heads, int* q_ctas, int* k_ctas) {
-    const int tiles = (T + kTokTile - 1) / kTokTile, budget = 148 * 4;
-    const int rows = std::max(1, q_heads + k_heads);
-    *q_ctas = q_heads ? std::max(1, std::min(tiles, (int)((long long)budget * q_heads / rows))) : 0;
+    const int tiles = (T + 1) / 2, budget = 148 * 2, rows = std::max(1, q_heads + k_heads);
     *k_ctas = k_heads ? std::max(1, std::min(tiles, (int)((long long)budget * k_heads / rows))) : 0;
+    *q_ctas = q_heads ? std::max(1, std::min(tiles, budget - *k_ctas)) : 0;
 }
 
 size_t head_grad_workspace_bytes(int T, int q_heads, int k_heads, int head_dim) {
@@ -435,15 +514,17 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
     p.items = items_of(p.dim, p.rot.dim, ve);
     p.lanes = std::min(32, pow2_at_least(p.items));
     p.groups = kHeadThreads / p.lanes;
+    while ((1 << p.lane_shift) < p.lanes) ++p.lane_shift;
     const dim3 grid(p.q_ctas + k_ctas);
+    const size_t smem = (size_t)kAhead * 4 * (ve == 1 ? 4 : 1) * kHeadThreads * ve * es;
     int rc = METEORA_OK;
     if (args.dtype == METEORA_BF16)
-        rc = ve == 8   ? launch_dependent<k_head_grad<__nv_bfloat16, 8, 1>>(grid, kHeadThreads, 0, st, p)
-             : ve == 4 ? launch_dependent<k_head_grad<__nv_bfloat16, 4, 1>>(grid, kHeadThreads, 0, st, p)
-                       : launch_dependent<k_head_grad<__nv_bfloat16, 1, 4>>(grid, kHeadThreads, 0, st, p);
+        rc = ve == 8   ? launch_dependent<k_head_grad<__nv_bfloat16, 8, 1>>(grid, kHeadThreads, smem, st, p)
+             : ve == 4 ? launch_dependent<k_head_grad<__nv_bfloat16, 4, 1>>(grid, kHeadThreads, smem, st, p)
+                       : launch_dependent<k_head_grad<__nv_bfloat16, 1, 4>>(grid, kHeadThreads, smem, st, p);
     else
-        rc = ve == 4 ? launch_dependent<k_head_grad<float, 4, 1>>(grid, kHeadThreads, 0, st, p)
-                     : launch_dependent<k_head_grad<float, 1, 4>>(grid, kHeadThreads, 0, st, p);
+        rc = ve == 4 ? launch_dependent<k_head_grad<float, 4, 1>>(grid, kHeadThreads, smem, st, p)
+                     : launch_dependent<k_head_grad<float, 1, 4>>(grid, kHeadThreads, smem, st, p);
     if (rc != METEORA_OK) return rc;
     const dim3 sums((x[1].heads ? 2 : 1) * ((p.dim + 31) / 32));
     return launch_dependent<k_gain_sums>(sums, 1024, 0, st, (const float*)part, p.q_ctas, k_ctas, p.dim, dq_gain, dk_gain);

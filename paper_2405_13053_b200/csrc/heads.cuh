@@ -60,17 +60,35 @@ template <typename E, int VE> struct HeadVec {
     }
 };
 
-// A head's entries as items of two vectors: item i < nr holds VE pairs of the rotated part (a and b their first and second
-// entries in the half layout, their first and last VE entries in the interleaved one), later items the rest.
+// A vector from global memory to a place in shared memory that this thread alone reads, on its way until row_wait (an entry of
+// two bytes is too small for that and arrives at once).
+template <typename Raw>
+__device__ __forceinline__ void row_copy(Raw* dst, const void* src) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+    else if constexpr (sizeof(Raw) >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(sizeof(Raw)) : "memory");
+    else *dst = *(const Raw*)src;
+}
+__device__ __forceinline__ void row_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void row_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// A head's entries as items of two vectors, so that a pair is in one thread and neighbouring lanes have neighbouring vectors:
+// item i < nr is vector i of either half of the rotated part, later items vectors of either half of the rest.  In the half
+// layout a pair is an entry of the first vector and the same one of the second, in the interleaved one two entries of a
+// vector (with vectors of one entry: the first and the second, 2 i and 2 i + 1).
 struct HeadItems {
-    int nr, half, dim, rot;
-    __device__ __forceinline__ HeadItems(int head_dim, int rot_dim, bool half_layout, int ve)
-        : nr(rot_dim / 2 / ve), half(half_layout), dim(head_dim), rot(rot_dim) {}
-    __device__ __forceinline__ int a(int i, int ve) const {
-        return i < nr ? (half ? i * ve : 2 * i * ve) : rot + 2 * (i - nr) * ve;
+    int nr, np, half, rot;
+    __device__ __forceinline__ HeadItems(int dim, int rot_dim, bool half_layout, int ve)
+        : nr(rot_dim / 2 / ve), np(((dim - rot_dim) / ve + 1) / 2), half(half_layout), rot(rot_dim) {}
+    __device__ __forceinline__ int a(int i, int ve) const { return i < nr ? (half || ve > 1 ? i * ve : 2 * i) : rot + (i - nr) * ve; }
+    __device__ __forceinline__ int b(int i, int ve) const {                  // at or past the head's end: there is none
+        return i < nr ? (half || ve > 1 ? rot / 2 + i * ve : 2 * i + 1) : rot + (np + i - nr) * ve;
     }
-    __device__ __forceinline__ int b(int i, int ve) const {
-        return i < nr ? (half ? rot / 2 + i * ve : (2 * i + 1) * ve) : rot + (2 * (i - nr) + 1) * ve;
+    // Where pair q's (cos, sin) stands: those of an item, first vector first, nr apart, so that lanes read neighbours.
+    __device__ __forceinline__ int table(int q, int ve) const {
+        if (half || ve == 1) return q % ve * nr + q / ve;
+        const int v = ve / 2, second = q >= rot / 4, r = second ? q - rot / 4 : q;
+        return (second * v + r % v) * nr + r / v;
     }
 };
 
@@ -96,10 +114,14 @@ __device__ __forceinline__ void turn_item(float (&a)[VE], float (&b)[VE], const 
     }
 }
 
-// Sum over the `lanes` (a power of two) neighbouring lanes that share a row.
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    return v;
+// Sums over the `lanes` (a power of two) neighbouring lanes that share a row.
+__device__ __forceinline__ void lanes_sum(float& a, float& b, int lanes) {
+    if (lanes == 8) {              // 64 to 128 entries in vectors of 8: the usual head
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o), b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+    } else {
+        for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o), b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+    }
 }
 
 // A batch over a paged cache, as the kernels take it.

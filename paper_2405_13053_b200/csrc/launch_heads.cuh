@@ -10,13 +10,14 @@ namespace meteora {
 // A launch that may be set up under the kernel ahead (every kernel here waits for it before it touches memory).
 template <auto kernel, typename... A>
 int launch_dependent(dim3 grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
-    if (smem > 48 * 1024) {
-        static std::atomic<bool> allowed[64];                       // per device; one size for all launches (the rest of 227 KB is for static arrays)
-        constexpr int kMaxSmem = 226 * 1024;
+    if (smem > 20 * 1024) {                                         // (48 KB with the static arrays, 25 KB at most)
+        static std::atomic<bool> allowed[64];                       // per device: all that static arrays leave, for launches of any size
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e == cudaSuccess && (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed))) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+            cudaFuncAttributes fa;
+            e = cudaFuncGetAttributes(&fa, kernel);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)fa.sharedSizeBytes);
             if (e == cudaSuccess && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
         }
         if (e != cudaSuccess) return cuda_status(e);
