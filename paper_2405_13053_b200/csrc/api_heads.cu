@@ -167,7 +167,7 @@ int meteora_head_norm_rotary(const meteora_heads_t* q, const meteora_heads_t* k,
 
 size_t meteora_head_norm_rotary_backward_workspace_bytes(int T, int q_heads, int k_heads, int head_dim) {
     if (T < 0 || q_heads < 1 || k_heads < 0 || head_dim < 1 || head_dim > METEORA_MAX_HEAD_DIM || q_heads > 65535 || k_heads > 65535) return 0;
-    return head_grad_workspace_bytes(T, q_heads, k_heads, head_dim);
+    return head_grad_workspace_bytes(T, head_dim);
 }
 
 int meteora_head_norm_rotary_backward(const meteora_heads_t* dq_out, const meteora_heads_t* dk_out, const meteora_heads_t* q,
@@ -194,7 +194,7 @@ int meteora_head_norm_rotary_backward(const meteora_heads_t* dq_out, const meteo
     if (!element_aligned(q_gain, dtype) || !element_aligned(k_gain, dtype) || (uintptr_t)dq_gain % 4 != 0 ||
         (uintptr_t)dk_gain % 4 != 0 || (uintptr_t)workspace % 16 != 0 || (rot && (uintptr_t)positions % (positions_64 ? 8 : 4) != 0))
         return METEORA_ERR_MISALIGNED;
-    if (workspace_bytes < head_grad_workspace_bytes(T, x[0].heads, x[1].heads, head_dim)) return METEORA_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < head_grad_workspace_bytes(T, head_dim)) return METEORA_ERR_WORKSPACE_TOO_SMALL;
     const HeadPassArgs args = {T, head_dim, dtype, positions, positions_64, rot, 1, eps, nullptr};
     const void* const gain[2] = {q_gain, has_k ? k_gain : nullptr};
     return launch_head_grad(dy, x, gain, dx, dq_gain, dk_gain, args, (float*)workspace, (cudaStream_t)stream);

@@ -19,13 +19,15 @@ __device__ __forceinline__ RowPieces row_pieces(const PieceSpace& s, int W, uint
     return RowPieces{(long long)(unit + c0) * s.rows + r, unit + c0 + n <= s.pieces ? n : 0};
 }
 
-// The pieces of one token's heads joined: the common maximum first, then their sum in order.  kWarps == 1: a warp takes
-// `heads_each` heads one after the other (a lane works out each one's pieces beforehand).  kWarps > 1, where the rows are
-// too few to hide one another's latency: a CTA per row, warp w sums pieces w, w + kWarps, ..., then the warps in order.
-template <typename E, int kWarps>
+// The pieces of one token's heads joined, kAhead of them at a time, by a running maximum like the pieces themselves, in their
+// order.  kWarps == 1: a warp takes `heads_each` heads one after the other (a lane works out each one's pieces beforehand).
+// kWarps > 1, where the rows are too few to hide one another's latency: a CTA per row, warp w joins pieces w, w + kWarps,
+// ..., then the warps in order.  kWide: heads of more than 128 entries.
+template <typename E, int kWarps, bool kWide>
 __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join(const __grid_constant__ AttendParams p, const int heads_each) {
-    __shared__ float4 s_acc[kWarps == 1 ? 1 : kWarps][64];
-    __shared__ float s_l[kWarps == 1 ? 1 : kWarps];
+    constexpr int kParts = kWide ? 2 : 1, kAhead = kWide ? 4 : 8;
+    __shared__ float4 s_acc[kWarps == 1 ? 1 : kWarps][32 * kParts];
+    __shared__ float2 s_ml[kWarps == 1 ? 1 : kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = kWarps == 1 ? 0 : warp;
     const int t = blockIdx.x, h0 = (kWarps == 1 ? (int)blockIdx.y * 4 + warp : (int)blockIdx.y) * heads_each;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -33,6 +35,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join
     if (h0 >= p.q_heads) return;
     const int b = sequence_of(p.batch, t, lane);
     if (b < 0) return;
+    const int W0 = p.prefix.total >= 0 ? p.prefix.total : p.total[0], W1 = p.total[1], first_tile = p.first_tile[b], first_unit = p.first_unit[b];
     const SequenceView s = sequence_view(p.batch, b);
     if (s.held < 0 || t >= s.first + s.tokens) return;
     RowPieces early = {}, late = {};
@@ -42,88 +45,97 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join
             const int i = t * p.group + g, rt = (int)((unsigned)i / (unsigned)p.prefix.rows), n_rt = row_tiles(p, p.batch.T, p.prefix.rows);
             const int tiles = (p.batch.prefix + (1 << p.prefix.shift) - 1) >> p.prefix.shift;
             const int unit = p.tc ? kv * n_rt + rt : rt * p.kv_heads + kv;
-            const int W = p.prefix.total >= 0 ? p.prefix.total : p.total[0];
-            early = row_pieces(p.prefix, W, (uint32_t)unit * (uint32_t)tiles, tiles, unit, i - rt * p.prefix.rows);
+            early = row_pieces(p.prefix, W0, (uint32_t)unit * (uint32_t)tiles, tiles, unit, i - rt * p.prefix.rows);
         }
         const int seen = min(s.held + (t - s.first) + 1, s.all);
         if (seen > 0) {
             const int i = (t - s.first) * p.group + g, rt = (int)((unsigned)i / (unsigned)p.own.rows), in = rt * p.kv_heads + kv;
             const int up = (1 << p.own.shift) - 1;
-            const uint32_t x0 = (uint32_t)p.first_tile[b] + (uint32_t)in * (uint32_t)((s.all + up) >> p.own.shift);
-            late = row_pieces(p.own, p.total[1], x0, (seen + up) >> p.own.shift, p.first_unit[b] + in, i - rt * p.own.rows);
+            const uint32_t x0 = (uint32_t)first_tile + (uint32_t)in * (uint32_t)((s.all + up) >> p.own.shift);
+            late = row_pieces(p.own, W1, x0, (seen + up) >> p.own.shift, first_unit + in, i - rt * p.own.rows);
         }
     }
+    const bool quads = p.dim % 4 == 0;
     for (int head = 0; head < heads_each && h0 + head < p.q_heads; ++head) {
         const int h = h0 + head;
         const int early_n = __shfl_sync(0xFFFFFFFFu, early.n, head), n = early_n + __shfl_sync(0xFFFFFFFFu, late.n, head);
         const long long early_row = __shfl_sync(0xFFFFFFFFu, early.row, head), late_row = __shfl_sync(0xFFFFFFFFu, late.row, head);
-        auto ml_of = [&](int i) {
-            return i < early_n ? p.prefix.ml[early_row + (long long)i * p.prefix.rows] : p.own.ml[late_row + (long long)(i - early_n) * p.own.rows];
-        };
-        float M = -INFINITY;
-        for (int i = lane; i < n; i += 32) M = fmaxf(M, ml_of(i).x);
+        float M = -INFINITY, L = 0.f;
+        float4 acc[kParts];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
-        const float base = M == -INFINITY ? 0.f : M;
-        const bool quads = p.dim % 4 == 0;
-        float L = 0.f;
-        float4 acc[2] = {};
-        constexpr int kAhead = 4;                    // pieces under way at a time
-        for (int i0 = part; i0 < n; i0 += 32 * kWarps) {
-            const int mine = i0 + lane * kWarps, count = min(32, (n - i0 + kWarps - 1) / kWarps);
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (mine < n) ml = ml_of(mine);
-            const float w = piece_factor(ml, base);
-            for (int j = 0; j < count; j += kAhead) {
-                float4 v[kAhead][2];
+        for (int c = 0; c < kParts; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i0 = part; i0 < n; i0 += kAhead * kWarps) {
+            float4 v[kAhead][kParts];
+            float2 ml[kAhead];
 #pragma unroll
-                for (int a = 0; a < kAhead; ++a) {
-                    const int i = i0 + (j + a) * kWarps;
-                    const float* o = i < early_n ? p.prefix.o + (early_row + (long long)i * p.prefix.rows) * p.dim
-                                                 : p.own.o + (late_row + (long long)(i - early_n) * p.own.rows) * p.dim;
+            for (int a = 0; a < kAhead; ++a) {
+                const int i = i0 + a * kWarps;
+                ml[a] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int e = (lane + 32 * c) * 4;
-                        v[a][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (j + a >= count || e >= p.dim) continue;
-                        if (quads) {
-                            v[a][c] = *reinterpret_cast<const float4*>(o + e);
-                        } else {
-                            v[a][c].x = o[e];
-                            if (e + 1 < p.dim) v[a][c].y = o[e + 1];
-                            if (e + 2 < p.dim) v[a][c].z = o[e + 2];
-                            if (e + 3 < p.dim) v[a][c].w = o[e + 3];
-                        }
-                    }
-                }
+                for (int c = 0; c < kParts; ++c) v[a][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i >= n) continue;
+                const bool is_early = i < early_n;
+                const long long row = is_early ? early_row + (long long)i * p.prefix.rows : late_row + (long long)(i - early_n) * p.own.rows;
+                const float* o = (is_early ? p.prefix.o : p.own.o) + row * p.dim;
+                ml[a] = (is_early ? p.prefix.ml : p.own.ml)[row];
 #pragma unroll
-                for (int a = 0; a < kAhead; ++a) {
-                    const float f = __shfl_sync(0xFFFFFFFFu, w, (j + a) & 31), fl = __shfl_sync(0xFFFFFFFFu, ml.y, (j + a) & 31);
-                    if (j + a >= count || f == 0.f) continue;            // (a piece in which the row sees nothing; NaN goes on)
-                    L = fmaf(f, fl, L);
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        acc[c].x = fmaf(f, v[a][c].x, acc[c].x);
-                        acc[c].y = fmaf(f, v[a][c].y, acc[c].y);
-                        acc[c].z = fmaf(f, v[a][c].z, acc[c].z);
-                        acc[c].w = fmaf(f, v[a][c].w, acc[c].w);
+                for (int c = 0; c < kParts; ++c) {
+                    const int e = (lane + 32 * c) * 4;
+                    if (e >= p.dim) continue;
+                    if (quads) {
+                        v[a][c] = *reinterpret_cast<const float4*>(o + e);
+                    } else {
+                        v[a][c].x = o[e];
+                        if (e + 1 < p.dim) v[a][c].y = o[e + 1];
+                        if (e + 2 < p.dim) v[a][c].z = o[e + 2];
+                        if (e + 3 < p.dim) v[a][c].w = o[e + 3];
                     }
                 }
             }
-        }
-        if (kWarps > 1) {                            // (one head)
+            float high = M;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) s_acc[part][lane + 32 * c] = acc[c];
-            if (lane == 0) s_l[part] = L;
+            for (int a = 0; a < kAhead; ++a) high = fmaxf(high, ml[a].x);
+            const float base = high == -INFINITY ? 0.f : high, f0 = M == -INFINITY ? (L != L ? L : 0.f) : exp2_fast(M - base);
+            M = high;
+            L = L * f0;
+#pragma unroll
+            for (int c = 0; c < kParts; ++c) acc[c] = make_float4(acc[c].x * f0, acc[c].y * f0, acc[c].z * f0, acc[c].w * f0);
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const float f = piece_factor(ml[a], base);
+                if (f == 0.f) continue;                              // (a piece in which the row sees nothing, or none; NaN goes on)
+                L = fmaf(f, ml[a].y, L);
+#pragma unroll
+                for (int c = 0; c < kParts; ++c) {
+                    acc[c].x = fmaf(f, v[a][c].x, acc[c].x);
+                    acc[c].y = fmaf(f, v[a][c].y, acc[c].y);
+                    acc[c].z = fmaf(f, v[a][c].z, acc[c].z);
+                    acc[c].w = fmaf(f, v[a][c].w, acc[c].w);
+                }
+            }
+        }
+        if (kWarps > 1) {                                            // (one head)
+#pragma unroll
+            for (int c = 0; c < kParts; ++c) s_acc[part][lane + 32 * c] = acc[c];
+            if (lane == 0) s_ml[part] = make_float2(M, L);
             __syncthreads();
             if (warp > 0) return;
+            float high = -INFINITY;
 #pragma unroll
-            for (int x = 1; x < kWarps; ++x) {
-                L += s_l[x];
+            for (int x = 0; x < kWarps; ++x) high = fmaxf(high, s_ml[x].x);
+            const float base = high == -INFINITY ? 0.f : high;
+            M = high, L = 0.f;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < kParts; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) {
+                const float f = piece_factor(s_ml[x], base);
+                if (f == 0.f) continue;
+                L = fmaf(f, s_ml[x].y, L);
+#pragma unroll
+                for (int c = 0; c < kParts; ++c) {
                     const float4 v = s_acc[x][lane + 32 * c];
-                    acc[c].x += v.x, acc[c].y += v.y, acc[c].z += v.z, acc[c].w += v.w;
+                    acc[c] = make_float4(fmaf(f, v.x, acc[c].x), fmaf(f, v.y, acc[c].y), fmaf(f, v.z, acc[c].z), fmaf(f, v.w, acc[c].w));
                 }
             }
         }
@@ -132,12 +144,13 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join
         E* const out = (E*)p.out + t * p.out_t + h * p.out_h;
         const bool wide = quads && ((uintptr_t)p.out | (uintptr_t)(p.out_t * sizeof(E)) | (uintptr_t)(p.out_h * sizeof(E))) % (4 * sizeof(E)) == 0;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < kParts; ++c) {
             const int e = (lane + 32 * c) * 4;
             const float v[4] = {acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv};
             if (e >= p.dim) continue;
             if (wide) {
-                HeadVec<E, 4>::store(out + e, HeadVec<E, 4>::pack(v));
+                const f32x2 pairs[2] = {make_pair2(v[0], v[1]), make_pair2(v[2], v[3])};
+                HeadVec<E, 4>::store(out + e, HeadVec<E, 4>::pack(pairs));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -249,10 +262,13 @@ template <typename E>
 static int launch_join(const AttendParams& p, cudaStream_t st) {
     const long long rows = (long long)p.batch.T * p.q_heads;
     if (rows <= 1184)                            // 8 CTAs per SM
-        return launch_dependent<k_attend_join<E, 8>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1);
+        return p.dim > 128 ? launch_dependent<k_attend_join<E, 8, true>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1)
+                           : launch_dependent<k_attend_join<E, 8, false>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1);
     const int each = (int)std::max(1LL, std::min(32LL, rows / (148 * 48)));       // heads per warp: as many as leave every SM 48 warps
     const int warps = (p.q_heads + each - 1) / each;
-    return launch_dependent<k_attend_join<E, 1>>(dim3(p.batch.T, (warps + 3) / 4), 128, 0, st, p, each);
+    const dim3 grid(p.batch.T, (warps + 3) / 4);
+    return p.dim > 128 ? launch_dependent<k_attend_join<E, 1, true>>(grid, 128, 0, st, p, each)
+                       : launch_dependent<k_attend_join<E, 1, false>>(grid, 128, 0, st, p, each);
 }
 
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,

@@ -7,7 +7,6 @@
 // the first of which are asked for before the angles.  Few tokens: one per CTA, its rows dealt over several CTAs.
 // Bound by HBM: every entry is read once and written once.
 #include <algorithm>
-#include <stdlib.h>
 
 #include "heads.cuh"
 #include "launch_heads.cuh"
@@ -25,7 +24,7 @@ struct HeadSeg {
     int heads, paged, turn;
 };
 
-constexpr int kMaxTokens = 8;      // of a CTA at a time
+constexpr int kMaxTokens = 4;      // of a CTA
 constexpr int kAhead = 2;          // rows of a group under way
 
 struct HeadPassParams {
@@ -42,7 +41,7 @@ template <typename E, int VE, int NI, bool kNorm>
 __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(const __grid_constant__ HeadPassParams p) {
     typedef HeadVec<E, VE> V;
     extern __shared__ __align__(16) uint8_t s_rows[];           // [kAhead][2 NI][threads] vectors
-    __shared__ float2 s_cs[kMaxTokens][kMaxPairs];
+    __shared__ __align__(16) float s_cs[kMaxTokens][2 * kMaxPairs];
     __shared__ int s_page[kMaxTokens], s_in_page[kMaxTokens];
     __shared__ long long s_pos[kMaxTokens];
     const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid >> p.lane_shift;
@@ -60,6 +59,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
         ob[n] = i < p.items ? it.b(i, VE) : p.dim;
     }
     typedef typename V::Raw Raw;
+    typedef typename V::P P;
     const auto place = [&](int slot, int v) { return reinterpret_cast<Raw*>(s_rows) + (slot * 2 * NI + v) * blockDim.x + tid; };
     const auto seg_of = [&](int r, int& h) {
         h = row_lo + r;
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
                                   : p.p64   ? __ldg((const long long*)p.positions + t0 + k)
                                             : (long long)__ldg((const int32_t*)p.positions + t0 + k);
             const int q = i - k * pairs;
-            s_cs[k][it.table(q, VE)] = rotary_pair(p.rot.turns[q], pos, p.inverse != 0, p.rot.scale);
+            store_angle<VE>(s_cs[k], it, q, rotary_pair(p.rot.turns[q], pos, p.inverse != 0, p.rot.scale));
         }
         __syncthreads();
     }
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
         int h = 0;
         const HeadSeg& g = p.seg[live ? seg_of(rr, h) : 0];
         Raw a[NI], b[NI];
-        float xa[NI][VE], xb[NI][VE];
+        P xa[NI][V::N], xb[NI][V::N];
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
             a[n] = live && oa[n] < p.dim ? *place(used % kAhead, 2 * n) : V::zero();
@@ -145,21 +145,24 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
         }
         ask();
         if (kNorm) {
-            float sum = 0.f, none = 0.f;
+            P sum2;
+            splat(sum2, 0.f);
 #pragma unroll
             for (int n = 0; n < NI; ++n)
 #pragma unroll
-                for (int j = 0; j < VE; ++j) sum = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], sum));
+                for (int j = 0; j < V::N; ++j) sum2 = fma_p(xa[n][j], xa[n][j], fma_p(xb[n][j], xb[n][j], sum2));
+            float sum = total(sum2), none = 0.f;
             lanes_sum(sum, none, p.lanes);
             if (g.gain) {
-                const float rs = 1.f / sqrtf(sum / (float)p.dim + p.eps);
+                P rs;
+                splat(rs, 1.f / sqrtf(sum / (float)p.dim + p.eps));
 #pragma unroll
                 for (int n = 0; n < NI; ++n) {
-                    float ga[VE], gb[VE];
+                    P ga[V::N], gb[V::N];
                     V::unpack(oa[n] < p.dim ? V::load((const E*)g.gain + oa[n]) : V::zero(), ga);
                     V::unpack(ob[n] < p.dim ? V::load((const E*)g.gain + ob[n]) : V::zero(), gb);
 #pragma unroll
-                    for (int j = 0; j < VE; ++j) xa[n][j] *= rs * ga[j], xb[n][j] *= rs * gb[j];
+                    for (int j = 0; j < V::N; ++j) xa[n][j] = mul_p(mul_p(xa[n][j], rs), ga[j]), xb[n][j] = mul_p(mul_p(xb[n][j], rs), gb[j]);
                 }
             }
         }
@@ -172,12 +175,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
                 if (oa[n] >= p.dim) continue;
                 const int i = lane + n * p.lanes;
                 const bool turn = g.turn && i < it.nr;
-                if (turn) {
-                    float2 cs[VE];
-#pragma unroll
-                    for (int j = 0; j < VE; ++j) cs[j] = s_cs[tt][j * it.nr + i];
-                    turn_item<VE>(xa[n], xb[n], cs, it.half);
-                }
+                if (turn) turn_item<VE>(xa[n], xb[n], s_cs[tt], it, i);
                 const bool same = !turn && !(kNorm && g.gain);           // bit for bit
                 V::store(dst + oa[n], same ? a[n] : V::pack(xa[n]));
                 if (ob[n] < p.dim) V::store(dst + ob[n], same ? b[n] : V::pack(xb[n]));
@@ -187,10 +185,14 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
     }
 }
 
-// Gradients of the norm with the rotation.  CTAs [0, q_ctas) take q, the others k; a CTA walks its share of the tokens,
-// kMaxTokens at a time (their angles by all its threads at once), and keeps its rows' sum of dn * n in registers: one row
-// of partial sums per CTA goes to the workspace, and k_gain_sums adds those up in their order.  Bound by HBM: x and dy
-// are read once, dx written once.
+// Gradients of the norm with the rotation.  A CTA takes an even share of the tokens, kGradTokens at a time (their angles by all
+// its threads at once); its first warps take the query heads, the others the key heads, as many as their heads ask for.
+// A group keeps its rows' sum of dn * n in registers: one row of partial sums per CTA and tensor goes to the workspace,
+// and k_gain_sums adds those up in their order.  With u = dn * x and c = r^3 mean(gain * u):
+//     dgain += r u,   dx = (gain r) dn - c x.
+// Bound by HBM (x and dy are read once, dx written once) and nearly as much by instructions, 240 for a thread's 16 entries.
+constexpr int kGradTokens = 16;
+
 struct HeadGradSeg {
     const void* dy;
     const void* x;
@@ -201,52 +203,55 @@ struct HeadGradSeg {
 };
 struct HeadGradParams {
     HeadGradSeg seg[2];
-    int q_ctas, groups, lanes, lane_shift, items;
+    int q_warps, lanes, lane_shift, items;
     int T, dim, p64;
     const void* positions;
     float eps;
-    float* part;             // [CTAs][dim]
+    float* part;             // [2][CTAs][dim]
     meteora_rotary_t rot;
 };
 
 template <typename E, int VE, int NI>
 __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_constant__ HeadGradParams p) {
     typedef HeadVec<E, VE> V;
-    __shared__ float2 s_cs[kMaxTokens][kMaxPairs];
-    __shared__ float s_sum[8][METEORA_MAX_HEAD_DIM];
+    typedef typename V::Raw Raw;
+    typedef typename V::P P;
+    constexpr int kWarps = kHeadThreads / 32;
+    __shared__ __align__(16) float s_cs[kGradTokens][2 * kMaxPairs];
+    __shared__ float s_sum[kWarps][METEORA_MAX_HEAD_DIM];
     extern __shared__ __align__(16) uint8_t s_rows[];           // [kAhead][4 NI][threads] vectors
-    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), group = tid >> p.lane_shift;
-    const bool is_k = (int)blockIdx.x >= p.q_ctas;
+    const int tid = threadIdx.x, lane = tid & (p.lanes - 1), warp = tid >> 5;
+    const bool is_k = warp >= p.q_warps;
     const HeadGradSeg& g = p.seg[is_k ? 1 : 0];
-    const int ctas = is_k ? gridDim.x - p.q_ctas : p.q_ctas, cta = is_k ? blockIdx.x - p.q_ctas : blockIdx.x;
-    const int t_lo = (int)((long long)p.T * cta / ctas), t_hi = (int)((long long)p.T * (cta + 1) / ctas);
+    const int group = (tid - (is_k ? p.q_warps * 32 : 0)) >> p.lane_shift;
+    const int groups = (is_k ? kWarps - p.q_warps : p.q_warps) * (32 >> p.lane_shift);
+    const int t_lo = (int)((long long)p.T * blockIdx.x / gridDim.x), t_hi = (int)((long long)p.T * (blockIdx.x + 1) / gridDim.x);
     const HeadItems it(p.dim, p.rot.dim, p.rot.layout == METEORA_ROTARY_HALF, VE);
     const int pairs = p.rot.dim / 2, heads = g.heads;
     const float inv_dim = 1.f / (float)p.dim;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int oa[NI], ob[NI];
-    typename V::Raw gain_a[NI], gain_b[NI];
-    float da[NI][VE], db[NI][VE];
+    Raw gain_a[NI], gain_b[NI];
+    P da[NI][V::N], db[NI][V::N];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
         const int i = lane + n * p.lanes;
         oa[n] = i < p.items ? it.a(i, VE) : p.dim;
         ob[n] = i < p.items ? it.b(i, VE) : p.dim;
-        gain_a[n] = oa[n] < p.dim ? V::load((const E*)g.gain + oa[n]) : V::zero();
-        gain_b[n] = ob[n] < p.dim ? V::load((const E*)g.gain + ob[n]) : V::zero();
+        gain_a[n] = heads > 0 && oa[n] < p.dim ? V::load((const E*)g.gain + oa[n]) : V::zero();
+        gain_b[n] = heads > 0 && ob[n] < p.dim ? V::load((const E*)g.gain + ob[n]) : V::zero();
 #pragma unroll
-        for (int j = 0; j < VE; ++j) da[n][j] = db[n][j] = 0.f;
+        for (int j = 0; j < V::N; ++j) splat(da[n][j], 0.f), splat(db[n][j], 0.f);
     }
     const auto step = [&](int& t, int& h) {
-        h += p.groups;
+        h += groups;
         while (h >= heads) h -= heads, ++t;
     };
-    typedef typename V::Raw Raw;
     const auto place = [&](int slot, int v) { return reinterpret_cast<Raw*>(s_rows) + (slot * 4 * NI + v) * kHeadThreads + tid; };
     // a group's rows: token t, head h; `far` runs kAhead rows ahead
-    int next_t = t_lo, next_h = group, asked = 0, used = 0;
-    while (next_h >= heads) next_h -= heads, ++next_t;
+    int next_t = heads > 0 ? t_lo : t_hi, next_h = group, asked = 0, used = 0;
+    while (heads > 0 && next_h >= heads) next_h -= heads, ++next_t;
     int far_t = next_t, far_h = next_h;
     const auto ask = [&]() {
         if (far_t < t_hi) {
@@ -270,24 +275,25 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
     };
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) ask();
-    for (int t0 = t_lo; t0 < t_hi; t0 += kMaxTokens) {
-        const int nt = min(kMaxTokens, t_hi - t0);
+    for (int t0 = t_lo; t0 < t_hi; t0 += kGradTokens) {
+        const int nt = min(kGradTokens, t_hi - t0);
         if (pairs > 0) {
             __syncthreads();
-            for (int i = tid; i < nt * pairs; i += blockDim.x) {
+            for (int i = tid; i < nt * pairs; i += kHeadThreads) {
                 const int k = i / pairs, q = i - k * pairs;
                 const long long pos = p.p64 ? __ldg((const long long*)p.positions + t0 + k)
                                             : (long long)__ldg((const int32_t*)p.positions + t0 + k);
-                s_cs[k][it.table(q, VE)] = rotary_pair(p.rot.turns[q], pos, true, p.rot.scale);
+                store_angle<VE>(s_cs[k], it, q, rotary_pair(p.rot.turns[q], pos, true, p.rot.scale));
             }
             __syncthreads();
         }
-        // (every group has a row in each round, or none: whole warps stay in the loop)
+        // (whole warps stay in the loop: the sums' shuffles need every lane)
         while (__any_sync(0xFFFFFFFFu, next_t < t0 + nt)) {
             const bool live = next_t < t0 + nt;
             const int t = next_t, h = next_h;
-            float xa[NI][VE], xb[NI][VE], ya[NI][VE], yb[NI][VE];
-            float sq = 0.f, dot = 0.f;
+            P xa[NI][V::N], xb[NI][V::N], ya[NI][V::N], yb[NI][V::N], sq2, dot2;
+            splat(sq2, 0.f);
+            splat(dot2, 0.f);
             row_wait<kAhead - 1>();
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
@@ -297,19 +303,14 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
                 V::unpack(in ? *place(used % kAhead, 4 * n + 1) : V::zero(), ya[n]);
                 V::unpack(in_b ? *place(used % kAhead, 4 * n + 2) : V::zero(), xb[n]);
                 V::unpack(in_b ? *place(used % kAhead, 4 * n + 3) : V::zero(), yb[n]);
-                if (i < it.nr && live) {
-                    float2 cs[VE];
-#pragma unroll
-                    for (int j = 0; j < VE; ++j) cs[j] = s_cs[t - t0][j * it.nr + i];
-                    turn_item<VE>(ya[n], yb[n], cs, it.half);
-                }
-                float ga[VE], gb[VE];
+                if (i < it.nr && live) turn_item<VE>(ya[n], yb[n], s_cs[t - t0], it, i);
+                P ga[V::N], gb[V::N];
                 V::unpack(gain_a[n], ga);
                 V::unpack(gain_b[n], gb);
 #pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    sq = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], sq));
-                    dot = fmaf(ga[j] * ya[n][j], xa[n][j], fmaf(gb[j] * yb[n][j], xb[n][j], dot));
+                for (int j = 0; j < V::N; ++j) {
+                    sq2 = fma_p(xa[n][j], xa[n][j], fma_p(xb[n][j], xb[n][j], sq2));
+                    dot2 = fma_p(ga[j], mul_p(ya[n][j], xa[n][j]), fma_p(gb[j], mul_p(yb[n][j], xb[n][j]), dot2));
                 }
             }
             if (live) {
@@ -317,23 +318,25 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
                 ++used;
                 ask();
             }
+            float sq = total(sq2), dot = total(dot2);
             lanes_sum(sq, dot, p.lanes);
             if (!live) continue;
-            const float rs = 1.f / sqrtf(sq * inv_dim + p.eps);
-            const float mean = dot * rs * inv_dim;                  // mean of gain * dn * n
+            const float r = 1.f / sqrtf(sq * inv_dim + p.eps);
+            P rs, c;
+            splat(rs, r);
+            splat(c, -r * r * r * (dot * inv_dim));
             E* dx = (E*)g.dx + t * g.dx_t + h * g.dx_h;
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
-                float ga[VE], gb[VE];
+                P ga[V::N], gb[V::N];
                 V::unpack(gain_a[n], ga);
                 V::unpack(gain_b[n], gb);
 #pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    const float na = xa[n][j] * rs, nb = xb[n][j] * rs;
-                    da[n][j] = fmaf(ya[n][j], na, da[n][j]);
-                    db[n][j] = fmaf(yb[n][j], nb, db[n][j]);
-                    xa[n][j] = rs * fmaf(ga[j], ya[n][j], -na * mean);
-                    xb[n][j] = rs * fmaf(gb[j], yb[n][j], -nb * mean);
+                for (int j = 0; j < V::N; ++j) {
+                    da[n][j] = fma_p(rs, mul_p(ya[n][j], xa[n][j]), da[n][j]);
+                    db[n][j] = fma_p(rs, mul_p(yb[n][j], xb[n][j]), db[n][j]);
+                    xa[n][j] = fma_p(mul_p(ga[j], rs), ya[n][j], mul_p(c, xa[n][j]));
+                    xb[n][j] = fma_p(mul_p(gb[j], rs), yb[n][j], mul_p(c, xb[n][j]));
                 }
                 if (oa[n] < p.dim) V::store(dx + oa[n], V::pack(xa[n]));
                 if (ob[n] < p.dim) V::store(dx + ob[n], V::pack(xb[n]));
@@ -341,28 +344,31 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
         }
     }
     // the groups' sums: inside a warp by shuffles, then warp by warp in order
+    float fa[NI][VE], fb[NI][VE];
 #pragma unroll
-    for (int n = 0; n < NI; ++n)
+    for (int n = 0; n < NI; ++n) {
+        memcpy(fa[n], da[n], sizeof(fa[n]));
+        memcpy(fb[n], db[n], sizeof(fb[n]));
 #pragma unroll
         for (int j = 0; j < VE; ++j)
             for (int o = p.lanes; o < 32; o <<= 1) {
-                da[n][j] += __shfl_xor_sync(0xFFFFFFFFu, da[n][j], o);
-                db[n][j] += __shfl_xor_sync(0xFFFFFFFFu, db[n][j], o);
+                fa[n][j] += __shfl_xor_sync(0xFFFFFFFFu, fa[n][j], o);
+                fb[n][j] += __shfl_xor_sync(0xFFFFFFFFu, fb[n][j], o);
             }
-    if ((tid & 31) < p.lanes) {
-#pragma unroll
-        for (int n = 0; n < NI; ++n)
+        if ((tid & 31) < p.lanes) {
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                if (oa[n] < p.dim) s_sum[tid >> 5][oa[n] + j] = da[n][j];
-                if (ob[n] < p.dim) s_sum[tid >> 5][ob[n] + j] = db[n][j];
+                if (oa[n] < p.dim) s_sum[warp][oa[n] + j] = fa[n][j];
+                if (ob[n] < p.dim) s_sum[warp][ob[n] + j] = fb[n][j];
             }
+        }
     }
     __syncthreads();
-    for (int d = tid; d < p.dim; d += blockDim.x) {
-        float v = s_sum[0][d];
-        for (int w = 1; w < (int)blockDim.x / 32; ++w) v += s_sum[w][d];
-        p.part[(size_t)blockIdx.x * p.dim + d] = v;
+    for (int i = tid; i < 2 * p.dim; i += kHeadThreads) {
+        const int which = i >= p.dim, d = i - which * p.dim, w0 = which ? p.q_warps : 0, w1 = which ? kWarps : p.q_warps;
+        float v = 0.f;
+        for (int w = w0; w < w1; ++w) v += s_sum[w][d];
+        p.part[((size_t)which * gridDim.x + blockIdx.x) * p.dim + d] = v;
     }
 }
 
@@ -458,7 +464,7 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     while ((1 << p.lane_shift) < p.lanes) ++p.lane_shift;
     // Up to four tokens per CTA; few tokens: the rows of each dealt over several CTAs.
     constexpr int kWave = 148 * 4;
-    p.tokens = getenv("TOK") ? atoi(getenv("TOK")) : std::min(4, (args.T + kWave - 1) / kWave);
+    p.tokens = std::min(4, (args.T + kWave - 1) / kWave);
     int rounds = (p.rows * p.lanes + kHeadThreads - 1) / kHeadThreads, split = 1;
     while (split < rounds && (long long)args.T * (split + 1) <= kWave) ++split;
     p.rows_per_cta = (p.rows + split - 1) / split;
@@ -472,18 +478,10 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     return norm ? launch_pass<float, true>(ve, grid, threads, p, st) : launch_pass<float, false>(ve, grid, threads, p, st);
 }
 
-// CTAs of the gradient kernel: two per SM (by registers), each with at least a few tokens; q and k get shares as their heads are.
-static void grad_ctas(int T, int q_heads, int k_heads, int* q_ctas, int* k_ctas) {
-    const int tiles = (T + 1) / 2, budget = 148 * 2, rows = std::max(1, q_heads + k_heads);
-    *k_ctas = k_heads ? std::max(1, std::min(tiles, (int)((long long)budget * k_heads / rows))) : 0;
-    *q_ctas = q_heads ? std::max(1, std::min(tiles, budget - *k_ctas)) : 0;
-}
+// CTAs of the gradient kernel: two per SM (by registers), a token each at least.
+static int grad_ctas(int T) { return std::max(1, std::min(T, 148 * 2)); }
 
-size_t head_grad_workspace_bytes(int T, int q_heads, int k_heads, int head_dim) {
-    int q = 0, k = 0;
-    grad_ctas(T, q_heads, k_heads, &q, &k);
-    return align_up((size_t)(q + k) * head_dim * 4, 256);
-}
+size_t head_grad_workspace_bytes(int T, int head_dim) { return align_up((size_t)2 * grad_ctas(T) * head_dim * 4, 256); }
 
 int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const void* const* gain, const meteora_heads_t* dx,
                      float* dq_gain, float* dk_gain, const HeadPassArgs& args, float* part, cudaStream_t st) {
@@ -491,8 +489,8 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
     for (int i = 0; i < 2; ++i)
         p.seg[i] = HeadGradSeg{dy[i].data, x[i].data, dx[i].data, gain[i], dy[i].stride_token, dy[i].stride_head, x[i].stride_token,
                                x[i].stride_head, dx[i].stride_token, dx[i].stride_head, x[i].heads};
-    int k_ctas = 0;
-    grad_ctas(args.T, x[0].heads, x[1].heads, &p.q_ctas, &k_ctas);
+    const int ctas = grad_ctas(args.T), warps = kHeadThreads / 32, all = x[0].heads + x[1].heads;
+    p.q_warps = x[1].heads == 0 ? warps : std::max(1, std::min(warps - 1, (warps * x[0].heads + all / 2) / all));
     p.T = args.T;
     p.dim = args.head_dim;
     p.p64 = args.positions_64;
@@ -513,9 +511,8 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
     });
     p.items = items_of(p.dim, p.rot.dim, ve);
     p.lanes = std::min(32, pow2_at_least(p.items));
-    p.groups = kHeadThreads / p.lanes;
     while ((1 << p.lane_shift) < p.lanes) ++p.lane_shift;
-    const dim3 grid(p.q_ctas + k_ctas);
+    const dim3 grid(ctas);
     const size_t smem = (size_t)kAhead * 4 * (ve == 1 ? 4 : 1) * kHeadThreads * ve * es;
     int rc = METEORA_OK;
     if (args.dtype == METEORA_BF16)
@@ -527,7 +524,7 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
                      : launch_dependent<k_head_grad<float, 1, 4>>(grid, kHeadThreads, smem, st, p);
     if (rc != METEORA_OK) return rc;
     const dim3 sums((x[1].heads ? 2 : 1) * ((p.dim + 31) / 32));
-    return launch_dependent<k_gain_sums>(sums, 1024, 0, st, (const float*)part, p.q_ctas, k_ctas, p.dim, dq_gain, dk_gain);
+    return launch_dependent<k_gain_sums>(sums, 1024, 0, st, (const float*)part, ctas, ctas, p.dim, dq_gain, dk_gain);
 }
 
 }  // namespace meteora

@@ -2,6 +2,8 @@
 // token of a batch stands in the paged cache.
 #pragma once
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace meteora {
@@ -32,8 +34,40 @@ template <> struct RawVec<8> { typedef uint2 type; };
 template <> struct RawVec<4> { typedef uint32_t type; };
 template <> struct RawVec<2> { typedef uint16_t type; };
 
+// Arithmetic on two fp32 in a register pair (one instruction each on this architecture), or on one.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 make_pair2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split_pair2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 mul_p(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma_p(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float mul_p(float a, float b) { return a * b; }
+__device__ __forceinline__ float fma_p(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ void splat(f32x2& r, float v) { r = make_pair2(v, v); }
+__device__ __forceinline__ void splat(float& r, float v) { r = v; }
+__device__ __forceinline__ float total(f32x2 v) {
+    float a, b;
+    split_pair2(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float total(float v) { return v; }
+
+// A vector of VE entries: as it lies in memory, and as VE / 2 register pairs (one float where it is one entry).
 template <typename E, int VE> struct HeadVec {
     typedef typename RawVec<VE * sizeof(E)>::type Raw;
+    typedef typename std::conditional<VE == 1, float, f32x2>::type P;
+    static constexpr int N = VE == 1 ? 1 : VE / 2;
     static __device__ __forceinline__ Raw load(const E* p) { return *reinterpret_cast<const Raw*>(p); }
     static __device__ __forceinline__ void store(E* p, const Raw& r) { *reinterpret_cast<Raw*>(p) = r; }
     static __device__ __forceinline__ Raw zero() {
@@ -41,21 +75,39 @@ template <typename E, int VE> struct HeadVec {
         memset(&r, 0, sizeof(r));
         return r;
     }
-    static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VE]) {
-        E e[VE];
-        memcpy(e, &r, sizeof(r));
+    static __device__ __forceinline__ void unpack(const Raw& r, P (&v)[N]) {
+        if constexpr (VE == 1) {
+            E e;
+            memcpy(&e, &r, sizeof(e));
+            v[0] = to_f32(e);
+        } else if constexpr (sizeof(E) == 2) {
+            uint32_t w[N];
+            memcpy(w, &r, sizeof(r));
 #pragma unroll
-        for (int i = 0; i < VE; ++i) v[i] = to_f32(e[i]);
-    }
-    static __device__ __forceinline__ Raw pack(const float (&v)[VE]) {
-        E e[VE];
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            if constexpr (sizeof(E) == 2) e[i] = __float2bfloat16_rn(v[i]);
-            else e[i] = v[i];
+            for (int i = 0; i < N; ++i) v[i] = bf16x2_to_f32x2(w[i]);
+        } else {
+            memcpy(v, &r, sizeof(r));
         }
+    }
+    static __device__ __forceinline__ Raw pack(const P (&v)[N]) {
         Raw r;
-        memcpy(&r, e, sizeof(r));
+        if constexpr (VE == 1) {
+            E e;
+            if constexpr (sizeof(E) == 2) e = __float2bfloat16_rn(v[0]);
+            else e = v[0];
+            memcpy(&r, &e, sizeof(e));
+        } else if constexpr (sizeof(E) == 2) {
+            uint32_t w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float a, b;
+                split_pair2(v[i], a, b);
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(b), "f"(a));
+            }
+            memcpy(&r, w, sizeof(r));
+        } else {
+            memcpy(&r, v, sizeof(r));
+        }
         return r;
     }
 };
@@ -84,32 +136,58 @@ struct HeadItems {
     __device__ __forceinline__ int b(int i, int ve) const {                  // at or past the head's end: there is none
         return i < nr ? (half || ve > 1 ? rot / 2 + i * ve : 2 * i + 1) : rot + (np + i - nr) * ve;
     }
-    // Where pair q's (cos, sin) stands: those of an item, first vector first, nr apart, so that lanes read neighbours.
+    // Where cos of pair q stands in a token's table, its sin `sin_off` further: an item's pairs two and two as (cos, cos, sin,
+    // sin), first vector first, 16 nr bytes apart, so that lanes read neighbours (vectors of one entry: as (cos, sin)).
     __device__ __forceinline__ int table(int q, int ve) const {
-        if (half || ve == 1) return q % ve * nr + q / ve;
-        const int v = ve / 2, second = q >= rot / 4, r = second ? q - rot / 4 : q;
-        return (second * v + r % v) * nr + r / v;
+        if (ve == 1) return 2 * q;
+        int i = q / ve, j = q % ve;
+        if (!half) {
+            const int v = ve / 2, second = q >= rot / 4, r = second ? q - rot / 4 : q;
+            i = r / v, j = second * v + r % v;
+        }
+        return ((j >> 1) * nr + i) * 4 + (j & 1);
     }
+    static __device__ __forceinline__ int sin_off(int ve) { return ve == 1 ? 1 : 2; }
 };
 
+// The angles of a token as it is needed: table[] as above, by `threads` threads of which this is `tid`.
 template <int VE>
-__device__ __forceinline__ void turn_item(float (&a)[VE], float (&b)[VE], const float2 (&cs)[VE], bool half) {
-    if (VE == 1 || half) {
+__device__ __forceinline__ void store_angle(float* table, const HeadItems& it, int q, float2 cs) {
+    float* const at = table + it.table(q, VE);
+    at[0] = cs.x;
+    at[HeadItems::sin_off(VE)] = cs.y;
+}
+
+// Item i's two vectors turned by its angles.
+template <int VE, typename P, int N>
+__device__ __forceinline__ void turn_item(P (&a)[N], P (&b)[N], const float* table, const HeadItems& it, int i) {
+    if constexpr (VE == 1) {
+        const float2 cs = *reinterpret_cast<const float2*>(table + 2 * i);
+        const float x = a[0], y = b[0];
+        a[0] = fmaf(y, -cs.y, __fmul_rn(x, cs.x));                 // (rounded as the pairs below are)
+        b[0] = fmaf(x, cs.y, __fmul_rn(y, cs.x));
+    } else if (it.half) {
 #pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const float x = a[j], y = b[j];
-            a[j] = x * cs[j].x - y * cs[j].y;
-            b[j] = y * cs[j].x + x * cs[j].y;
+        for (int j = 0; j < N; ++j) {
+            const float4 t = *reinterpret_cast<const float4*>(table + (j * it.nr + i) * 4);
+            const f32x2 c = make_pair2(t.x, t.y), s = make_pair2(t.z, t.w), m = make_pair2(-t.z, -t.w), x = a[j], y = b[j];
+            a[j] = fma_p(y, m, mul_p(x, c));
+            b[j] = fma_p(x, s, mul_p(y, c));
         }
     } else {
+        // an entry pair is (x, y) -> (x c - y s, y c + x s) = (x, y) * (c, c) + (y, x) * (-s, s)
 #pragma unroll
-        for (int j = 0; j + 1 < VE; j += 2) {
-            const float2 ca = cs[j / 2], cb = cs[VE / 2 + j / 2];
-            const float x = a[j], y = a[j + 1], z = b[j], w = b[j + 1];
-            a[j] = x * ca.x - y * ca.y;
-            a[j + 1] = y * ca.x + x * ca.y;
-            b[j] = z * cb.x - w * cb.y;
-            b[j + 1] = w * cb.x + z * cb.y;
+        for (int j = 0; j < N; ++j) {
+            const float4 t = *reinterpret_cast<const float4*>(table + (j * it.nr + i) * 4);      // of pairs 2 j and 2 j + 1 of the item
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int e = 2 * j + k;                           // of the first vector's pairs, then the second's
+                P& v = e < N ? a[e < N ? e : 0] : b[e < N ? 0 : e - N];
+                const float c = k ? t.y : t.x, s = k ? t.w : t.z;
+                float x, y;
+                split_pair2(v, x, y);
+                v = fma_p(make_pair2(y, x), make_pair2(-s, s), mul_p(v, make_pair2(c, c)));
+            }
         }
     }
 }

@@ -53,7 +53,7 @@ struct HeadPassArgs {
     const BatchView* batch;
 };
 int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args, cudaStream_t st);
-size_t head_grad_workspace_bytes(int T, int q_heads, int k_heads, int head_dim);
+size_t head_grad_workspace_bytes(int T, int head_dim);
 int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const void* const* gain, const meteora_heads_t* dx,
                      float* dq_gain, float* dk_gain, const HeadPassArgs& args, float* part, cudaStream_t st);
 

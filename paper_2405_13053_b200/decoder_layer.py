@@ -1,15 +1,17 @@
 """A LLaMA3-8B decoder layer around the seven MeteoRA linears (Sec. 3.1: a MeteoRA module replaces each of q, k, v,
 o, gate, up and down of every block; Sec. 3.2: every one of them has its own gate and adapters).
 
-Only the seven linears are the library's; everything else (RMSNorm, rotary position embedding, grouped-query
-attention with 32 query and 8 key/value heads of 128, SwiGLU, the two residual adds) runs as plain torch ops and
-exists so that each linear consumes the real upstream activation:
+The seven linears are the library's, and with a `PagedCache` so is what stands between q/k/v and o: the rotation with
+the append to the cache, and the attention that reads it.  Everything else (RMSNorm, grouped-query attention with 32
+query and 8 key/value heads of 128 without such a cache, SwiGLU, the two residual adds) runs as plain torch ops and exists
+so that each linear consumes the real upstream activation:
 
     n1 = RMSNorm(x);  q, k, v = linears(n1);  rotary(q, k);  a = attention(q, [cache; k], [cache; v])
     h  = x + o(a);    n2 = RMSNorm(h);        y = h + down(SiLU(gate(n2)) * up(n2))
 
-Two modes: a decode batch (one new token for each of B sequences, keys and values of `context` earlier tokens in a
-cache) and a prefill (one sequence of T tokens, causal attention).  The linears go through `linears`, an object
+Three modes: a decode batch (one new token for each of B sequences, keys and values of `context` earlier tokens in a
+cache), a prefill (one sequence of T tokens, causal attention), and a batch over a paged cache (any number of new tokens of
+each of B sequences behind a prefix that they share).  The linears go through `linears`, an object
 with `one(name, x)` and `many(names, x)`: `LibraryLinears` calls the CUDA library (modules that share their input
 as one group call), tests put a CPU reference in its place, and `FixedLinears` returns preallocated tensors so
 that the rest of the layer can be timed alone.
@@ -104,13 +106,57 @@ class FixedLinears:
         return [self.out[n] for n in names]
 
 
-def layer_forward(x: torch.Tensor, norms: Dict[str, torch.Tensor], linears, positions: torch.Tensor,
-                  cache_k: Optional[torch.Tensor] = None, cache_v: Optional[torch.Tensor] = None) -> torch.Tensor:
+class PagedCache:
+    """One layer's keys and values of B sequences of up to `tokens` own tokens each, in pages, behind a prefix of `prefix_len`
+    tokens that all of them share.  `lengths` are the sequences' own tokens in the cache: a step appends at them and
+    attends, `advance` moves them on afterwards (tensors on the device: a captured step goes on as they grow)."""
+
+    def __init__(self, B: int, tokens: int, prefix_len: int = 0, page_size: int = 64, dtype=torch.bfloat16, device="cuda"):
+        from . import binding
+        self.mb, self.prefix_len = binding, prefix_len
+        width, n_prefix = -(-tokens // page_size), -(-prefix_len // page_size)
+        shape = (B * width + n_prefix, N_KV_HEADS, page_size, HEAD_DIM)
+        self.k, self.v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        pages = torch.arange(shape[0], dtype=torch.int32, device=device)
+        self.page_table, self.prefix_pages = pages[:B * width].view(B, width), pages[B * width:]
+        self.lengths = torch.zeros(B, dtype=torch.int32, device=device)
+        self.rot = binding.meteora_rotary_init(HEAD_DIM, ROPE_THETA)
+        self.workspaces: Dict[int, torch.Tensor] = {}
+
+    def append_prefix(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Keys (not yet rotated) and values [prefix_len, N_KV_HEADS, HEAD_DIM] of the prefix."""
+        none = torch.zeros(1, dtype=torch.int32, device=k.device)
+        first = torch.tensor([0, k.shape[0]], dtype=torch.int32, device=k.device)
+        self.mb.meteora_cache_append(k, v, self.k, self.v, self.prefix_pages.view(1, -1), none, self.rot, cu_tokens=first)
+
+    def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_tokens: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Appends the new tokens' k (rotated) and v [T, N_KV_HEADS, HEAD_DIM] and returns the attention of their q."""
+        T = q.shape[0]
+        q = self.mb.meteora_cache_append(k, v, self.k, self.v, self.page_table, self.lengths, self.rot, cu_tokens=cu_tokens,
+                                         prefix_len=self.prefix_len, q=q)
+        if T not in self.workspaces:            # made on first use, so that a CUDA graph can be captured afterwards
+            self.workspaces[T] = self.mb.meteora_prefix_attention_workspace(q, self.k, self.page_table, self.prefix_len)
+        return self.mb.meteora_prefix_attention(q, self.k, self.v, self.page_table, self.lengths, self.prefix_pages, self.prefix_len,
+                                                cu_tokens=cu_tokens, workspace=self.workspaces[T])
+
+    def advance(self, new) -> None:
+        """`new`: tokens of the step per sequence (a number, or int32 [B])."""
+        self.lengths += new
+
+
+def layer_forward(x: torch.Tensor, norms: Dict[str, torch.Tensor], linears, positions: Optional[torch.Tensor] = None,
+                  cache_k: Optional[torch.Tensor] = None, cache_v: Optional[torch.Tensor] = None,
+                  paged: Optional[PagedCache] = None, cu_tokens: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x[T, HIDDEN].  With a cache ([B, N_KV_HEADS, context, HEAD_DIM], B = T): decode, token t is the next token of
-    sequence t at position positions[t].  Without: prefill of one sequence, causal attention over the T tokens."""
+    sequence t at position positions[t].  With `paged`: the T new tokens of its sequences, sequence b's from cu_tokens[b]
+    on (None: one each), at the positions that follow from its lengths.  Without: prefill of one sequence, causal
+    attention over the T tokens."""
     T = x.shape[0]
     n1 = rms_norm(x, norms["input"])
     q, k, v = linears.many(("q", "k", "v"), n1)
+    if paged is not None:
+        a = paged.attend(q.view(T, N_HEADS, HEAD_DIM), k.view(T, N_KV_HEADS, HEAD_DIM), v.view(T, N_KV_HEADS, HEAD_DIM), cu_tokens)
+        return _behind_attention(x, a.view(T, N_HEADS * HEAD_DIM), norms, linears)
     q = rotary(q.view(T, N_HEADS, HEAD_DIM), positions)
     k = rotary(k.view(T, N_KV_HEADS, HEAD_DIM), positions)
     v = v.view(T, N_KV_HEADS, HEAD_DIM)
@@ -123,6 +169,10 @@ def layer_forward(x: torch.Tensor, norms: Dict[str, torch.Tensor], linears, posi
         a = torch.nn.functional.scaled_dot_product_attention(q.transpose(0, 1)[None], k.transpose(0, 1)[None],
                                                              v.transpose(0, 1)[None], is_causal=True, enable_gqa=True)
         a = a[0].transpose(0, 1).reshape(T, N_HEADS * HEAD_DIM)
+    return _behind_attention(x, a, norms, linears)
+
+
+def _behind_attention(x, a, norms, linears) -> torch.Tensor:
     h = x + linears.one("o", a.contiguous())
     n2 = rms_norm(h, norms["post_attention"])
     gate, up = linears.many(("gate", "up"), n2)
