@@ -202,11 +202,16 @@ static AttendPlan plan_attend(const AttendSizes& z, void* workspace) {
     p.by_group = fixed_div((uint32_t)p.group);
     p.by_page = fixed_div((uint32_t)z.page_size);
     plan.mma = z.dtype == METEORA_BF16 && z.head_dim % 8 == 0;
-    p.tc = prefix_tc_supported(z);
     const long long rows = (long long)z.T * p.group, mean = std::max(1, z.B > 0 ? z.T / z.B : 1);    // mean: new tokens of a sequence
-    // 64 rows at a time where there are more than 16: of the prefix all of them, of own tokens a sequence's mean
+    // More than 16 rows at a time: on the tensor cores where these take the shape, else 64; of the prefix all rows, of own
+    // tokens a sequence's mean.  Own tokens of up to 64 rows per sequence stay with the 64-row kernel where the keys are few:
+    // a unit of the other costs about 20 us / SM to start and end (us, own tokens alone, 64-row kernel / tensor cores: 16
+    // sequences of 55 rows, 355 keys, 40 heads 80 / 109; 32 of 64 rows, 516 keys 56 / 76; 32 of 128 rows 91 / 79; 64 of 24 rows,
+    // 1024 keys 555 / 441; 2 of 8000 rows, 2000 keys 820 / 231).
+    p.tc = z.prefix_len > 0 && attend_tc_supported(z, rows);
+    p.own_tc = (mean * p.group > 64 || (long long)z.table_width * z.page_size >= 1024) && attend_tc_supported(z, mean * p.group);
     p.prefix.rows = p.tc ? kPrefixRows : plan.mma && rows > 16 ? 64 : 16;
-    p.own.rows = plan.mma && mean * p.group > 16 ? 64 : 16;
+    p.own.rows = p.own_tc ? kPrefixRows : plan.mma && mean * p.group > 16 ? 64 : 16;
     plan.together = !p.tc && z.prefix_len > 0 && p.prefix.rows == p.own.rows;
     const auto units = [&](int r) { return (rows + r - 1) / r * z.kv_heads; };
     size_t off = kHeaderBytes;
@@ -221,17 +226,24 @@ static AttendPlan plan_attend(const AttendSizes& z, void* workspace) {
         s.ml = (float2*)take((size_t)s.pieces * s.rows * 8);
     };
     const long long prefix_units = z.prefix_len > 0 ? units(p.prefix.rows) : 0;
-    set_kernel(p.own, z, plan.mma);
+    const auto set_tc = [](PieceSpace& s) {      // one CTA per SM
+        s.shift = 7;
+        s.least_shift = 0;
+        s.workers = 148;
+        s.total = -1;
+    };
+    if (p.own_tc) set_tc(p.own);
+    else set_kernel(p.own, z, plan.mma);
     space(p.own, units(p.own.rows) + (long long)z.B * z.kv_heads + (plan.together ? prefix_units : 0));
     if (plan.together) {
         p.prefix = p.own;
     } else if (z.prefix_len > 0) {
-        set_kernel(p.prefix, z, plan.mma);
         if (p.tc) {
-            p.prefix.shift = 7;
-            p.prefix.least_shift = 0;
+            set_tc(p.prefix);
             p.prefix.total = (int)(prefix_units * ((z.prefix_len + kPrefixTile - 1) / kPrefixTile));
             p.prefix.workers = std::max(1, std::min(148, p.prefix.total));
+        } else {
+            set_kernel(p.prefix, z, plan.mma);
         }
         space(p.prefix, prefix_units);
     }
@@ -291,12 +303,13 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
         a.with_prefix = prefix;
         a.with_own = own;
         a.here = own ? p.own : p.prefix;
+        if (own ? p.own_tc : p.tc) return launch_attend_tc(a, own, st);
         if (plan.mma) return p.dim <= 64 ? launch_mma<64>(a, st) : p.dim <= 128 ? launch_mma<128>(a, st) : launch_mma<256>(a, st);
         if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
         return launch_dependent<k_attend_simt<float>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
     };
     int rc = METEORA_OK;
-    if (z.prefix_len > 0 && !plan.together) rc = p.tc ? launch_prefix_tc(p, st) : pieces(true, false);
+    if (z.prefix_len > 0 && !plan.together) rc = pieces(true, false);
     if (rc == METEORA_OK) rc = pieces(plan.together, true);
     if (rc != METEORA_OK) return rc;
     return z.dtype == METEORA_BF16 ? launch_join<__nv_bfloat16>(p, st) : launch_join<float>(p, st);

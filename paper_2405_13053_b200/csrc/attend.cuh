@@ -74,7 +74,7 @@ struct AttendParams {
     FixedDiv by_group, by_page;
     float scale_log2;              // scale * log2(e)
     PieceSpace prefix, own;        // (the same where one launch has both)
-    int tc;                        // the prefix runs on the tensor-core kernel
+    int tc, own_tc;                // the prefix / the own tokens run on the tensor-core kernel
     // of this launch (not the tensor-core kernel's): which parts it has, its pieces
     int with_prefix, with_own;
     PieceSpace here;
@@ -201,7 +201,8 @@ struct Walk {
     }
 };
 
-// The start of a worker's share, worked out by its CTA of 128 threads and kWorkers workers (this thread's is `mine`).  For the
+// The start of a worker's share, worked out by the first 128 threads of its CTA, which all call it, for its kWorkers workers
+// (this thread's is `mine`).  For the
 // join CTA 0 leaves the totals, and whoever has a sequence's first tile its start.
 template <int kWorkers>
 __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
@@ -211,7 +212,7 @@ __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
     __shared__ int s_units[kWarps], s_b[kWorkers], s_unit[kWorkers];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int B = p.with_own ? p.batch.B : 0, per = (B + kThreadsOf - 1) / kThreadsOf;
-    const int b_lo = min(B, tid * per), b_hi = min(B, b_lo + per);
+    const int b_lo = min(B, tid * per), b_hi = tid < kThreadsOf ? min(B, b_lo + per) : b_lo;
     Walk w;
     long long before = 0;          // tiles and units of the prefix
     int units_before = 0;
@@ -238,7 +239,7 @@ __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
         const int v = __shfl_up_sync(0xFFFFFFFFu, u, o);
         if (lane >= o) x64 += y, u += v;
     }
-    if (lane == 31) s_tiles[warp] = x64, s_units[warp] = u;
+    if (lane == 31 && warp < kWarps) s_tiles[warp] = x64, s_units[warp] = u;
     if (tid < kWorkers) s_b[tid] = -2;
     __syncthreads();
     long long W64 = before;
@@ -260,7 +261,7 @@ __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
         if (p.with_own) p.total[1] = (int)W;
     }
     if (tid < kWorkers && start(c0 + tid) < before) s_b[tid] = -1, s_x[tid] = 0, s_unit[tid] = 0;
-    if (x < start(c0 + kWorkers) && x + min(tiles, kMost) > start(c0)) {
+    if (b_hi > b_lo && x < start(c0 + kWorkers) && x + min(tiles, kMost) > start(c0)) {
         for (int b = b_lo; b < b_hi; ++b) {
             w.enter(p, b);
             if (w.tiles == 0 || w.n_rt == 0) continue;

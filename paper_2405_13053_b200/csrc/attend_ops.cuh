@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t round_pair(float& a, float& b) {
 template <int DP> struct AttendWarpShape {
     static constexpr int kChunks = DP / 8;                         // 16-byte chunks of a row
     static constexpr int kTileBytes = kWarpTile * DP * 2;          // keys or values of a tile
-    static constexpr int kStages = 3;
+    static constexpr int kStages = DP == 128 ? 2 : 3;
     static constexpr int kInfos = 4;                               // tiles described: one more than kStages
     static constexpr int kWarpBytes = 2 * kStages * kTileBytes;
     static constexpr int kBytes = 1024 + 4 * (kWarpBytes + kInfos * 40 + kStages * 8);

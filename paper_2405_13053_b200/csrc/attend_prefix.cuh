@@ -1,8 +1,10 @@
-// The shared prefix of a bf16 batch on the tensor cores: rows of all sequences against the prefix's keys (attend.cuh has
-// the mathematics and where the pieces go).  Included by wgemm_tcgen05.cu after the device helpers it uses.
+// Attention on the tensor cores, for bf16 caches (attend.cuh has the mathematics and where the pieces go): the shared prefix, rows of
+// all sequences against its keys, and (kOwn) own tokens of sequences that bring more than 16 rows.
+// Included by wgemm_tcgen05.cu after the device helpers it uses.
 //
-// A unit of work is 256 rows (token, head of one kv head's group) x the prefix, in tiles of 128 keys; the tiles are dealt to
-// one CTA per SM in even shares (units of one kv head follow one another: their CTAs read the same keys at about the same time).
+// A unit of work is 256 rows (token, head of one kv head's group) x their keys, in tiles of 128 keys; the tiles are dealt to
+// one CTA per SM in even shares (the prefix's units of one kv head follow one another: their CTAs read the same keys at about the
+// same time).
 //
 // The rows are two tiles of 128 with a softmax group of eight warps each, two threads per row, 64 of a tile's keys each.
 // Scores S = Q K^T go to TMEM, the group turns them into weights 2^(s - m), rounded to bf16 and stored over the scores they
@@ -15,8 +17,10 @@
 // and spares nearly all rescaling of O.  The two threads of a row need the same m: their warps exchange one word that says
 // whether any of their rows needs a new one, and only then the maxima themselves (through unused columns of TMEM).
 //
-// A page that is not there and the keys behind the prefix's end count as -inf, and their values are zeroed in shared memory:
-// what the cache holds there (an infinity, a NaN) would pass a weight of 0.
+// A page that is not there and the keys behind the last count as -inf, and their values are zeroed in shared memory: what
+// the cache holds there (an infinity, a NaN) would pass a weight of 0.  So would a value that is no finite number of an own
+// token that only some of the rows see: in tiles with such tokens those values are zeroed too, and added to the rows that
+// see them when the unit is done.
 #pragma once
 
 #include "attend.cuh"
@@ -25,14 +29,17 @@ namespace meteora {
 
 constexpr int kPfxKeys = kPrefixTile, kPfxRows = kPrefixRows;
 constexpr int kPfxThreads = 576;                     // warp 0: copies, warp 1: products, 16 warps of softmax
+constexpr int kPfxUnits = 16;                        // units described (more than the ring holds)
 constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
 
 template <int D> struct PrefixShape {
     static constexpr int kTileBytes = kPfxKeys * D * 2;
     static constexpr int kStages = D == 128 ? 5 : 11;              // of keys or values of one tile
     static constexpr int kBarOff = (2 + kStages) * kTileBytes;     // barriers, then page masks, TMEM slot
-    static constexpr int kBars = 2 * kStages + 19;
-    static constexpr int kSmem = 1024 + kBarOff + kBars * 8 + kPfxMasks * 4 + 16 * 4 + 16;
+    static constexpr int kBars = 2 * kStages + 19 + kPfxUnits;
+    static constexpr int kWords = kBarOff + kBars * 8;             // page masks [kPfxMasks], growth [16], zeroed [2 words], TMEM slot, then the units
+    static constexpr int kUnitOff = (kWords + (kPfxMasks + 19) * 4 + 15) / 16 * 16;
+    static constexpr int kSmem = 1024 + kUnitOff + kPfxUnits * 48;
 };
 
 struct PrefixTcParams {
@@ -102,9 +109,42 @@ __device__ __forceinline__ unsigned long long fma2_of(unsigned long long a, unsi
     return r;
 }
 
-template <int D>
+// The units of a CTA's share, one after the other; the copies' warp walks them and leaves each one's description.
+struct __align__(16) TcUnit {
+    int id, b, h, row0;                              // id < 0: no more; b: sequence or -1; rows [row0, row0 + rows) of its
+    int rows, first, held, tile0;                    // tokens' and heads'; first token; own tokens held before
+    int count, hi, none[2];                          // tiles of keys, from tile0; keys that any of the rows sees
+    // keys that the row-th row of the unit sees
+    __device__ __forceinline__ int limit(const AttendParams& p, int row) const {
+        return b < 0 ? hi : min(hi, held + (int)p.by_group.of((unsigned)(row0 + row)) + 1);
+    }
+};
+template <bool kOwn> struct TcUnits {
+    Walk w;
+    int x, x_hi, unit_tiles, pair_tiles, rows_all;
+    __device__ __forceinline__ bool next(const AttendParams& p, TcUnit& u) {
+        if (kOwn) {
+            if (w.left <= 0) return false;
+            u.id = w.unit, u.b = w.b, u.h = w.h, u.row0 = w.rt * kPfxRows, u.rows = min(kPfxRows, w.tokens * p.group - u.row0);
+            u.first = w.first, u.held = w.held, u.tile0 = w.tile, u.hi = w.hi;
+            u.count = min(w.left, (w.hi + kPfxKeys - 1) / kPfxKeys - w.tile);
+            w.left -= u.count;
+            w.tile += u.count;
+            w.settle(p);
+            return true;
+        }
+        if (x >= x_hi) return false;
+        u.id = x / unit_tiles, u.b = -1, u.h = u.id / pair_tiles, u.row0 = u.id % pair_tiles * kPfxRows, u.rows = min(kPfxRows, rows_all - u.row0);
+        u.first = 0, u.held = 0, u.tile0 = x - u.id * unit_tiles, u.hi = p.batch.prefix;
+        u.count = min(x_hi, (u.id + 1) * unit_tiles) - x;
+        x += u.count;
+        return true;
+    }
+};
+
+template <int D, bool kOwn>
 __global__ void __launch_bounds__(kPfxThreads, 1)
-k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixTcParams pp) {
+k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixTcParams pp) {
     typedef PrefixShape<D> S;
     constexpr int kHalves = D / 64;
     const AttendParams& p = pp.a;
@@ -113,15 +153,13 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     uint8_t* const base_ptr = smem_raw + (base - raw);
     const uint32_t s_q = base, ring = base + 2 * S::kTileBytes;
     const uint32_t bar_full = base + S::kBarOff, bar_free = bar_full + S::kStages * 8, bar_s = bar_free + S::kStages * 8, bar_p = bar_s + 16,
-                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_x = bar_q + 16, bar_tail = bar_x + 64;
-    volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kBarOff + S::kBars * 8);
+                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_x = bar_q + 16, bar_tail = bar_x + 64, bar_u = bar_tail + 8;
+    volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kWords);
     volatile uint32_t* const s_grow = s_mask + kPfxMasks;          // [tile of rows][half][quarter]
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kBarOff + S::kBars * 8 + kPfxMasks * 4 + 16 * 4);
+    volatile uint32_t* const s_odd = s_grow + 16;                  // the unit in which values were zeroed, + 1
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kWords + (kPfxMasks + 18) * 4);
+    int4* const s_unit = reinterpret_cast<int4*>(base_ptr + S::kUnitOff);
     const int warp = warp_id(), lane = threadIdx.x & 31;
-    const int unit_tiles = (p.batch.prefix + kPfxKeys - 1) / kPfxKeys;
-    const Shares shares((uint32_t)p.prefix.total, gridDim.x);
-    const int x_lo = (int)shares.start(blockIdx.x), x_hi = (int)shares.start(blockIdx.x + 1);
-    const int rows_all = p.batch.T * p.group, pair_tiles = (rows_all + kPfxRows - 1) / kPfxRows;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -137,6 +175,8 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         }
         for (int i = 0; i < 8; ++i) mbar_init(bar_x + i * 8, 2);
         mbar_init(bar_tail, 1);
+        for (int i = 0; i < kPfxUnits; ++i) mbar_init(bar_u + i * 8, 1);
+        *s_odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -152,20 +192,48 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bool ok = true;
     int where = 0;
+    const PieceSpace& space = kOwn ? p.own : p.prefix;
+    TcUnits<kOwn> units;
+    if (kOwn) {
+        units.w = start_walk<1>(p, 0);
+    } else {
+        const Shares shares((uint32_t)p.prefix.total, gridDim.x);
+        units.x = (int)shares.start(blockIdx.x), units.x_hi = (int)shares.start(blockIdx.x + 1);
+        units.unit_tiles = (p.batch.prefix + kPfxKeys - 1) / kPfxKeys;
+        units.rows_all = p.batch.T * p.group, units.pair_tiles = (units.rows_all + kPfxRows - 1) / kPfxRows;
+    }
 
     if (warp == 0) {
         // ---- copies: K then V of every tile, page by page
-        int n = 0, tails = 0, done = 0;
-        for (int x = x_lo; x < x_hi && ok; ++x, ++done) {
-            const int unit = x / unit_tiles, tile = x - unit * unit_tiles, h = unit / pair_tiles;
-            const int key0 = tile * kPfxKeys, boxes = kPfxKeys >> pp.box_shift;
-            const int limit = min(kPfxKeys, p.batch.prefix - key0);            // keys of the tile that there are
+        int n = 0, tails = 0, done = 0, told = 0;
+        const auto tell = [&](const TcUnit& u) {
+            if (lane == 0) {
+                const int slot = told % kPfxUnits;
+                const int4* const from = reinterpret_cast<const int4*>(&u);
+                s_unit[slot * 3] = from[0], s_unit[slot * 3 + 1] = from[1], s_unit[slot * 3 + 2] = from[2];
+                mbar_arrive(bar_u + slot * 8);
+            }
+            ++told;
+        };
+        TcUnit u = {};
+        while (ok && units.next(p, u)) {
+        tell(u);
+        const PageList pages = page_list(p.batch, u.b);
+        for (int r = lane; r < u.rows; r += 32) {                              // the unit's queries towards L2
+            const int j = (int)p.by_group.of((unsigned)(u.row0 + r)), g = u.row0 + r - j * p.group;
+            const char* src = (const char*)((const __nv_bfloat16*)p.q + (u.first + j) * p.q_t + (int64_t)(u.h * p.group + g) * p.q_h);
+#pragma unroll
+            for (int c = 0; c < D * 2; c += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + c));
+        }
+        for (int tile = u.tile0; tile < u.tile0 + u.count && ok; ++tile, ++done) {
+            const int key0 = tile * kPfxKeys, boxes = kPfxKeys >> pp.box_shift, h = u.h;
+            const int limit = min(kPfxKeys, u.hi - key0);                      // keys of the tile that there are
             long long page = -1;
             int at = 0;
             if (lane < boxes && lane * pp.box_rows < limit) {
-                const int key = key0 + lane * pp.box_rows, slot = key / p.batch.page;
+                const int key = key0 + lane * pp.box_rows, slot = (int)p.by_page.of((unsigned)key);
                 at = key - slot * p.batch.page;
-                page = __ldg(p.batch.prefix_pages + slot);
+                if (slot < pages.n) page = __ldg(pages.pages + slot);
                 if (page < 0 || page >= p.batch.n_pages) page = -1;
             }
             const uint32_t mask = __ballot_sync(0xFFFFFFFFu, page >= 0);
@@ -207,12 +275,15 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 }
             }
         }
+        }
+        u.id = -1;
+        tell(u);
         if (!ok)                                                               // copies in flight land before the CTA leaves
             for (int q = max(0, n - S::kStages); q < n; ++q) mbar_wait_warp(bar_full + (q % S::kStages) * 8, (q / S::kStages) & 1);
     } else if (warp == 1) {
         // ---- products
         const uint32_t idesc_s = instr_desc_bf16(kPfxKeys), idesc_o = instr_desc_bf16(D) | (1u << 16);
-        int n = 0, tiles_of[2] = {0, 0}, segs_of[2] = {0, 0};
+        int n = 0, tiles_of[2] = {0, 0}, segs_of[2] = {0, 0}, heard = 0;
         auto scores = [&](int i, uint32_t k_tile) {
             if (elect_one()) {
 #pragma unroll
@@ -241,9 +312,15 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             __syncwarp();
         };
         auto wait_full = [&](int i) { return mbar_wait_warp(bar_full + (i % S::kStages) * 8, (i / S::kStages) & 1); };
-        for (int x = x_lo; x < x_hi && ok;) {
-            const int unit = x / unit_tiles, row0 = unit % pair_tiles * kPfxRows;
-            const int count = min(x_hi, (unit + 1) * unit_tiles) - x, active = rows_all - row0 > 128 ? 2 : 1;
+        while (ok) {
+            ok = mbar_wait_warp(bar_u + heard % kPfxUnits * 8, heard / kPfxUnits & 1);
+            if (!ok) {
+                where = 11;
+                break;
+            }
+            const TcUnit& u = reinterpret_cast<const TcUnit*>(s_unit)[heard++ % kPfxUnits];
+            if (u.id < 0) break;
+            const int count = u.count, active = u.rows > 128 ? 2 : 1;
             ok = wait_full(n);
             for (int i = 0; i < active && ok; ++i) ok = mbar_wait_warp(bar_q + i * 8, segs_of[i] & 1);
             if (!ok) {
@@ -278,7 +355,6 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 if (j + 1 < count) release((n + 2) % S::kStages);
             }
             for (int i = 0; i < active; ++i) ++segs_of[i];
-            x += count;
         }
     } else {
         // ---- softmax: four groups of four warps, (tile of rows, half of the keys); a warp's TMEM lanes are those of its number mod 4
@@ -289,7 +365,7 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         volatile uint32_t* const grow_mine = s_grow + (i * 2 + half) * 4 + quad;
         volatile uint32_t* const grow_other = s_grow + (i * 2 + 1 - half) * 4 + quad;
         constexpr int kCols = kPfxKeys / 2, kPart = D / 4;         // scores of a thread; entries of O that leave at a time
-        int tiles = 0, segs = 0, done = 0, pairs = 0;
+        int tiles = 0, segs = 0, done = 0, pairs = 0, heard = 0;
         // The two warps of 32 rows wait for each other.
         auto meet = [&]() {
             __syncwarp();
@@ -298,14 +374,21 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             ++pairs;
             return met;
         };
-        for (int x = x_lo; x < x_hi && ok;) {
-            const int unit = x / unit_tiles, h = unit / pair_tiles, row0 = unit % pair_tiles * kPfxRows;
-            const int count = min(x_hi, (unit + 1) * unit_tiles) - x, first_tile = x - unit * unit_tiles;
-            if (i == 1 && rows_all - row0 <= 128) {                            // no rows for the second tile
-                x += count;
+        while (ok) {
+            ok = mbar_wait_warp(bar_u + heard % kPfxUnits * 8, heard / kPfxUnits & 1);
+            if (!ok) {
+                where = 12;
+                break;
+            }
+            const TcUnit u = reinterpret_cast<const TcUnit*>(s_unit)[heard++ % kPfxUnits];
+            if (u.id < 0) break;
+            const int count = u.count, h = u.h;
+            if (i == 1 && u.rows <= 128) {                                     // no rows for the second tile
                 done += count;
                 continue;
             }
+            const int row = i * 128 + quad * 32 + lane, lim = min(u.hi, row < u.rows ? u.limit(p, row) : 0);     // keys this row sees
+            const int lim_all = u.limit(p, 0);                                 // and the first one, so all of them
             // queries: a warp 16 of the 32 rows, each row's chunks by neighbouring lanes
             {
                 constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks;
@@ -314,10 +397,10 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 uint4 v[16 / kAtOnce];
 #pragma unroll
                 for (int q = 0; q < 16 / kAtOnce; ++q) {
-                    const int at = row0 + i * 128 + quad * 32 + half * 16 + q * kAtOnce + lane / kChunks;
+                    const int at = i * 128 + quad * 32 + half * 16 + q * kAtOnce + lane / kChunks;
                     v[q] = make_uint4(0u, 0u, 0u, 0u);
-                    if (at < rows_all) {
-                        const int t = (int)p.by_group.of((unsigned)at), g = at - t * p.group;
+                    if (at < u.rows) {
+                        const int j = (int)p.by_group.of((unsigned)(u.row0 + at)), g = u.row0 + at - j * p.group, t = u.first + j;
                         const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + t * p.q_t + (int64_t)(h * p.group + g) * p.q_h + c * 8;
                         if (((uintptr_t)src & 15) == 0) {
                             v[q] = *reinterpret_cast<const uint4*>(src);
@@ -347,15 +430,22 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 }
                 tc_fence_after();
                 const uint32_t mask = s_mask[done % kPfxMasks];
-                const int limit = min(kPfxKeys, p.batch.prefix - (first_tile + j) * kPfxKeys) - half * kCols;
+                const int key0 = (u.tile0 + j) * kPfxKeys + half * kCols;       // of this half
                 float s[kCols];
                 tmem_ld32(t_s + half * kCols, s);
                 tmem_ld32(t_s + half * kCols + 32, s + 32);
                 tmem_wait_ld();
-                if (limit < kCols || __popc(mask) < (kPfxKeys >> pp.box_shift)) {
+                if (key0 + kCols > lim_all) {                                  // keys that this row does not see
+                    const int n = lim - key0;
 #pragma unroll
-                    for (int k = 0; k < kCols; ++k)
-                        if (k >= limit || !(mask >> ((half * kCols + k) >> pp.box_shift) & 1u)) s[k] = -INFINITY;
+                    for (int k = 0; k < kCols; ++k) s[k] = k < n ? s[k] : -INFINITY;
+                }
+                if (__popc(mask) < (kPfxKeys >> pp.box_shift)) {               // keys of pages that are not there
+#pragma unroll
+                    for (int k = 0; k < kCols; k += 8)
+                        if (!(mask >> ((half * kCols + k) >> pp.box_shift) & 1u))
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) s[k + q] = -INFINITY;
                 }
                 float top[2] = {max3(s[0], s[2], s[4]), max3(s[1], s[3], s[5])};
 #pragma unroll
@@ -419,6 +509,27 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 unpair2(sum2[0], a, b);
                 l += a + b;
                 tmem_wait_st();
+                if (kOwn && lim_all < u.hi && (u.tile0 + j + 1) * kPfxKeys > lim_all) {
+                    // keys that some rows do not see: values that are no finite numbers become zeros (by both tiles of rows alike)
+                    const int st = (2 * done + 1) % S::kStages;
+                    if (!mbar_wait_warp(bar_full + st * 8, (2 * done + 1) / S::kStages & 1)) {
+                        ok = false, where = 10;
+                        break;
+                    }
+                    uint4* const v = reinterpret_cast<uint4*>(base_ptr + (ring - base) + st * S::kTileBytes);
+                    for (int e = (half * 4 + quad) * 32 + lane; e < S::kTileBytes / 16; e += 256) {
+                        uint4 x = v[e];
+                        uint32_t* const w = reinterpret_cast<uint32_t*>(&x);
+                        bool odd = false;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if ((w[q] & 0x7F80u) == 0x7F80u) w[q] &= 0xFFFF0000u, odd = true;
+                            if ((w[q] & 0x7F800000u) == 0x7F800000u) w[q] &= 0xFFFFu, odd = true;
+                        }
+                        if (odd) v[e] = x, *s_odd = (uint32_t)u.id + 1u;           // (the other tile of rows finds zeros)
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_p + i * 8);
@@ -431,8 +542,8 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             tc_fence_after();
             // kPart entries at a time through the place of the queries, so that a store is whole lines of several rows; a
             // thread's own row straight from its registers takes 32 of them
-            const size_t piece = (size_t)(unit + (int)blockIdx.x) * kPfxRows + i * 128 + quad * 32;
-            const int rows_here = min(32, rows_all - row0 - i * 128 - quad * 32);
+            const size_t piece = (size_t)(u.id + (int)blockIdx.x) * kPfxRows + i * 128 + quad * 32;
+            const int rows_here = u.id + (int)blockIdx.x < space.pieces ? min(32, u.rows - i * 128 - quad * 32) : 0;
             // the row's sum: the halves' sums through a column of TMEM that no product uses any more
             if (half == 1) {
                 tmem_st1(t_s + 64, l);
@@ -446,7 +557,7 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             tc_fence_after();
             if (half == 0) {
                 l += tmem_ld1(t_s + 64);
-                if (lane < rows_here) p.prefix.ml[piece + lane] = make_float2(ref, l);
+                if (lane < rows_here) space.ml[piece + lane] = make_float2(ref, l);
             }
             uint8_t* const turn = base_ptr + i * S::kTileBytes + (D == 128 ? half * (kPfxKeys * 128) : half * 2048) + quad * 4096;
             constexpr int kQuads = kPart / 4, kRowsAtOnce = 32 / kQuads;       // 16-byte pieces of a row
@@ -455,6 +566,24 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 float o[kPart];
 #pragma unroll
                 for (int q = 0; q < kPart; q += 16) tmem_ld16(t_o + half * (D / 2) + c + q, *reinterpret_cast<float(*)[16]>(o + q));
+                if (kOwn && *s_odd == (uint32_t)u.id + 1u) {                 // what was zeroed, to the rows that see it
+                    const PageList pages = page_list(p.batch, u.b);
+                    const int from = max(u.tile0, lim_all / kPfxKeys) * kPfxKeys, to = min(lim, (u.tile0 + count) * kPfxKeys);
+                    for (int key = from; key < to; ++key) {
+                        const long long at = key_row(pages, p.batch, p.by_page, key, p.kv_heads, h);
+                        const __nv_bfloat16* v = (const __nv_bfloat16*)p.v + at * D + half * (D / 2) + c;
+                        for (int q = 0; at >= 0 && q < kPart; q += 2) {
+                            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + q);
+                            const float a = (w & 0x7F80u) == 0x7F80u ? __uint_as_float(w << 16) : 0.f;
+                            const float b = (w & 0x7F800000u) == 0x7F800000u ? __uint_as_float(w & 0xFFFF0000u) : 0.f;
+                            if (a != 0.f || b != 0.f) {
+#pragma unroll
+                                for (int e = 0; e < kPart; e += 2)
+                                    if (e == q) o[e] += a, o[e + 1] += b;
+                            }
+                        }
+                    }
+                }
 #pragma unroll
                 for (int q = 0; q < kQuads; ++q)
                     *reinterpret_cast<float4*>(turn + lane * (kPart * 4) + ((q ^ (lane & (kQuads - 1))) << 4)) =
@@ -464,7 +593,7 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 for (int q = 0; q < kQuads; ++q) {
                     const int rr = q * kRowsAtOnce + lane / kQuads, e = lane % kQuads;
                     const float4 v = *reinterpret_cast<const float4*>(turn + rr * (kPart * 4) + ((e ^ (rr & (kQuads - 1))) << 4));
-                    if (rr < rows_here) *reinterpret_cast<float4*>(p.prefix.o + (piece + rr) * D + half * (D / 2) + c + e * 4) = v;
+                    if (rr < rows_here) *reinterpret_cast<float4*>(space.o + (piece + rr) * D + half * (D / 2) + c + e * 4) = v;
                 }
                 __syncwarp();
             }
@@ -475,7 +604,6 @@ k_prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             }
             if (lane == 0) mbar_arrive(bar_ofree + i * 8);
             ++segs;
-            x += count;
         }
     }
     if (!ok && where && lane == 0) {

@@ -20,7 +20,7 @@
 namespace meteora {
 
 template <int DP, bool kTma>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(128, DP == 256 ? 1 : 3)
 k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendParams p, const int box_shift) {
     typedef AttendWarpShape<DP> S;
     extern __shared__ uint8_t smem_raw[];

@@ -62,9 +62,9 @@ struct AttendSizes {
     long long n_pages;
     meteora_dtype_t dtype;
 };
-// wgemm_tcgen05.cu: the prefix on the tensor cores
-bool prefix_tc_supported(const AttendSizes& z);
-int launch_prefix_tc(const AttendParams& p, cudaStream_t st);
+// wgemm_tcgen05.cu: units of `rows` rows on the tensor cores, the prefix's or the own tokens'
+bool attend_tc_supported(const AttendSizes& z, long long rows);
+int launch_attend_tc(const AttendParams& p, bool own, cudaStream_t st);
 // and units of up to 16 rows (entries of a head padded to `padded`: 64, 128 or 256)
 int launch_attend_warp(const AttendParams& p, int padded, cudaStream_t st);
 size_t attend_workspace_bytes(const AttendSizes& z);

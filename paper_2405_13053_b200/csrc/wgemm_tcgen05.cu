@@ -3062,10 +3062,9 @@ static int prefix_box_rows(int page_size) {
     return r;
 }
 
-bool prefix_tc_supported(const AttendSizes& z) {
-    const long long rows = (long long)z.T * (z.q_heads / z.kv_heads);
-    return z.dtype == METEORA_BF16 && (z.head_dim == 64 || z.head_dim == 128) && prefix_box_rows(z.page_size) >= 8 && z.prefix_len > 0 && rows > 16 &&
-           rows < (1LL << 31) - kPfxRows && z.n_pages > 0 && z.n_pages * z.kv_heads < (1LL << 31);
+bool attend_tc_supported(const AttendSizes& z, long long rows) {
+    return z.dtype == METEORA_BF16 && (z.head_dim == 64 || z.head_dim == 128) && prefix_box_rows(z.page_size) >= 8 && rows > 16 && z.n_pages > 0 &&
+           z.n_pages * z.kv_heads < (1LL << 31);
 }
 
 // Tensor map of a cache [pages * kv_heads][page_size][D] as (64 entries, keys, blocks of 64 entries, planes): a box is `rows` keys and
@@ -3081,12 +3080,13 @@ static int get_cache_map(const void* ptr, int D, int page_size, long long planes
     return r == CUDA_SUCCESS ? METEORA_OK : METEORA_ERR_CUDA;
 }
 
-template <int D>
-static int launch_prefix_tc_d(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixTcParams& pp, cudaStream_t st) {
-    return launch_dependent<k_prefix_tc<D>>(dim3(pp.a.prefix.workers), kPfxThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
+template <int D, bool kOwn>
+static int launch_attend_tc_d(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixTcParams& pp, cudaStream_t st) {
+    const int ctas = kOwn ? pp.a.own.workers : pp.a.prefix.workers;
+    return launch_dependent<k_attend_tc<D, kOwn>>(dim3(ctas), kPfxThreads, smem_with_tmem(PrefixShape<D>::kSmem, 512), st, tk, tv, pp);
 }
 
-int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
+int launch_attend_tc(const AttendParams& p, bool own, cudaStream_t st) {
     PrefixTcParams pp = {};
     pp.a = p;
     pp.box_rows = prefix_box_rows(p.batch.page);
@@ -3097,7 +3097,8 @@ int launch_prefix_tc(const AttendParams& p, cudaStream_t st) {
     int rc;
     if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, 1, &tk)) != METEORA_OK) return rc;
     if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, pp.box_rows, 1, &tv)) != METEORA_OK) return rc;
-    return p.dim == 64 ? launch_prefix_tc_d<64>(tk, tv, pp, st) : launch_prefix_tc_d<128>(tk, tv, pp, st);
+    if (own) return p.dim == 64 ? launch_attend_tc_d<64, true>(tk, tv, pp, st) : launch_attend_tc_d<128, true>(tk, tv, pp, st);
+    return p.dim == 64 ? launch_attend_tc_d<64, false>(tk, tv, pp, st) : launch_attend_tc_d<128, false>(tk, tv, pp, st);
 }
 
 template <int DP, bool kTma>

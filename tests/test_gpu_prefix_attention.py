@@ -98,6 +98,9 @@ CASES = {
     "no_prefix": dict(B=3, new=[1, 4, 2], held=[100, 0, 31], page=16, prefix=0, H=6, K=2, D=128, dtype=BF16, behind=3),
     "chunk": dict(B=3, new=[33, 1, 70], held=[0, 90, 31], page=16, prefix=130, H=8, K=2, D=128, dtype=BF16),
     "chunk_behind": dict(B=4, new=[5, 0, 40, 9], held=[3, 50, 0, 64], page=64, prefix=65, H=5, K=5, D=64, dtype=BF16, pad=(3,), behind=5),
+    "prompts": dict(B=3, new=[300, 41, 150], held=[0, 130, 257], page=16, prefix=70, H=8, K=4, D=128, dtype=BF16, behind=2),
+    "prompts_no_prefix": dict(B=2, new=[513, 1], held=[0, 64], page=64, prefix=0, H=2, K=2, D=64, dtype=BF16, drop=((0, 3), (0, 8))),
+    "few_rows_long_keys": dict(B=2, new=[24, 20], held=[1100, 900], page=8, prefix=200, H=3, K=3, D=64, dtype=BF16, pad=()),
     "chunk_wide_heads": dict(B=2, new=[20, 37], held=[10, 0], page=32, prefix=100, H=4, K=2, D=256, dtype=BF16),
     "decode_wide_heads": dict(B=3, new=[1] * 3, held=[130, 2, 64], page=32, prefix=200, H=4, K=2, D=256, dtype=BF16),
     "odd_page": dict(B=3, new=[2, 1, 3], held=[50, 0, 23], page=24, prefix=75, H=12, K=4, D=80, dtype=BF16),
@@ -166,10 +169,11 @@ def test_scale_and_workspace():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("K,D", [(2, 128), (4, 64), (2, 256)])
-def test_values_that_are_no_numbers_stay_with_the_rows_that_see_them(dtype, K, D):
+@pytest.mark.parametrize("K,D,more", [(2, 128, 0), (4, 64, 0), (2, 256, 0), (2, 128, 260), (4, 64, 330)])
+def test_values_that_are_no_numbers_stay_with_the_rows_that_see_them(dtype, K, D, more):
     """NaN in the value of a later token, in one sequence's own pages, in one query: only the rows that see them change."""
-    new, held, prefix = [40, 3, 1], [10, 5, 20], 90
+    new, held, prefix = [40 + more, 3, 1], [10, 5, 20], 90
+    n = new[0]
     s = make(B=3, new=new, held=held, page=16, prefix=prefix, H=4, K=K, D=D, dtype=dtype, nan=False)
     want = call(s)
     bad = dict(s, vc=s["vc"].clone(), kc=s["kc"].clone(), q=s["q"].clone())
@@ -181,9 +185,9 @@ def test_values_that_are_no_numbers_stay_with_the_rows_that_see_them(dtype, K, D
     got = call(bad)
     a, b = hu.to64(got), hu.to64(want)
     hit = np.zeros(a.shape, bool)
-    hit[17:40, :, 3], hit[30:40, :, D - 1] = True, True
-    hit[40:43, :, 0] = True                                          # sequence 1: every token sees its third
-    hit[43], hit[5, 1] = True, True
+    hit[17:n, :, 3], hit[30:n, :, D - 1] = True, True
+    hit[n:n + 3, :, 0] = True                                        # sequence 1: every token sees its third
+    hit[n + 3], hit[5, 1] = True, True
     assert np.array_equal(a[~hit], b[~hit]) or np.abs(a - b)[~hit].max() <= 2.0 ** -7 * np.abs(b).max()
     assert np.isfinite(a[~hit]).all() and not np.isfinite(a[hit]).any()
 
