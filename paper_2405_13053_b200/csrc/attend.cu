@@ -303,6 +303,7 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
         a.with_prefix = prefix;
         a.with_own = own;
         a.here = own ? p.own : p.prefix;
+        a.beside = own && !prefix && z.prefix_len > 0;
         if (own ? p.own_tc : p.tc) return launch_attend_tc(a, own, st);
         if (plan.mma) return p.dim <= 64 ? launch_mma<64>(a, st) : p.dim <= 128 ? launch_mma<128>(a, st) : launch_mma<256>(a, st);
         if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);

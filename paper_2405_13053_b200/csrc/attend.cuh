@@ -75,14 +75,25 @@ struct AttendParams {
     float scale_log2;              // scale * log2(e)
     PieceSpace prefix, own;        // (the same where one launch has both)
     int tc, own_tc;                // the prefix / the own tokens run on the tensor-core kernel
-    // of this launch (not the tensor-core kernel's): which parts it has, its pieces
-    int with_prefix, with_own;
+    // of this launch: which parts it has, its pieces, and whether it may run beside the launch ahead (the prefix's)
+    int with_prefix, with_own, beside;
     PieceSpace here;
     int32_t* total;                // [2] tiles of the launch with the prefix / with the own tokens
     int32_t* first_tile;           // [B] where a sequence's own tiles start in their launch
     int32_t* first_unit;           // [B] and its units
     int32_t* status;
 };
+
+// The order of launches.  A kernel waits for the launches ahead before it touches memory; the own tokens' launch behind the
+// prefix's needs nothing of that one, which has let it start after its own wait: it waits at its end instead, so that the
+// join, which waits for this launch alone, finds both done.
+__device__ __forceinline__ void launch_begins(const AttendParams& p) {
+    if (!p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void launch_ends(const AttendParams& p) {
+    if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 // What a sequence has: own tokens [0, held + tokens), of which the table holds `all`.
 struct SequenceView {

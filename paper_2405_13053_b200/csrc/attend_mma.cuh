@@ -37,8 +37,7 @@ __global__ void __launch_bounds__(128) k_attend_mma(const __grid_constant__ Atte
     int* const s_info = reinterpret_cast<int*>(s_off + S::kOffs * kAttendTile);        // [kOffs][kInfoInts]
     const uint32_t kv0 = (uint32_t)__cvta_generic_to_shared(s_kv), q0 = (uint32_t)__cvta_generic_to_shared(s_qs);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    launch_begins(p);
     Walk w = start_walk<1>(p, 0);                                  // runs ahead: where the places of keys are looked up
     const int cta = (int)blockIdx.x;
 
@@ -291,6 +290,7 @@ __global__ void __launch_bounds__(128) k_attend_mma(const __grid_constant__ Atte
         if (more) store_place(next_row);
     }
     cp_async_wait<0>();
+    launch_ends(p);
 }
 
 }  // namespace meteora

@@ -188,8 +188,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);    // S of both tiles, then O of both
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    launch_begins(p);
     bool ok = true;
     int where = 0;
     const PieceSpace& space = kOwn ? p.own : p.prefix;
@@ -614,6 +613,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     __syncthreads();
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    launch_ends(p);
 }
 
 }  // namespace meteora

@@ -27,8 +27,7 @@ __global__ void __launch_bounds__(128) k_attend_simt(const __grid_constant__ Att
     float* const s_f = s_p + kAttendTile * 20;                 // [16] factors of the sums so far, then [16] the rows' limits
     long long* const s_off = reinterpret_cast<long long*>(s_f + 32);
     const int tid = threadIdx.x, lane = tid & 31;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    launch_begins(p);
     Walk w = start_walk<1>(p, 0);
     const int ra = (tid >> 4) * 2, kq = tid & 15;              // rows ra, ra + 1 and keys kq + 16 i
     while (w.left > 0) {
@@ -185,6 +184,7 @@ __global__ void __launch_bounds__(128) k_attend_simt(const __grid_constant__ Att
                 if (r < rows_used) p.here.o[(piece + r) * p.dim + e] = o[i][r];
         }
     }
+    launch_ends(p);
 }
 
 }  // namespace meteora

@@ -38,11 +38,13 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    launch_begins(p);
     Walk w = start_walk<4>(p, warp);                               // runs ahead: the tile whose page is asked for
     const int worker = (int)blockIdx.x * 4 + warp;
-    if (w.left <= 0) return;
+    if (w.left <= 0) {
+        launch_ends(p);
+        return;
+    }
 
     auto swz = [](int row, int chunk) { return (uint32_t)((chunk >> 3) * (kWarpTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)); };
     constexpr int kCopies = kWarpTile * S::kChunks / 32;           // 16-byte copies of a lane, for keys and values each
@@ -356,6 +358,7 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
         for (int i = max(0, fetched - S::kStages); i < fetched; ++i) mbar_wait_warp(bar + i % S::kStages * 8, i / S::kStages & 1);   // copies under way land
     }
+    launch_ends(p);
 }
 
 }  // namespace meteora
