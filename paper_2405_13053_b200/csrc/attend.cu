@@ -188,7 +188,7 @@ static void set_kernel(PieceSpace& s, const AttendSizes& z, bool mma) {
     const bool warps = mma && s.rows == kWarpRows;
     s.workers = warps ? 4 * ctas : ctas;
     s.shift = warps ? 4 : 6;
-    s.least_shift = warps ? 2 : 0;               // (64 keys: a piece of fewer costs the join more than it saves)
+    s.least_shift = warps ? 1 : 0;               // (32 keys: a piece of fewer costs the join more than it saves)
     s.total = -1;
 }
 
