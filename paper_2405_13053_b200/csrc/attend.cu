@@ -1,7 +1,7 @@
 // Attention for a batch whose sequences share a prefix, over a paged cache: the plan of a call and its launches.
 #include <algorithm>
 
-#include "attend_mma.cuh"
+#include "attend_ops.cuh"
 #include "attend_simt.cuh"
 #include "launch_heads.cuh"
 
@@ -264,12 +264,6 @@ size_t attend_workspace_bytes(const AttendSizes& z) {
     return plan.fits ? plan.bytes : 0;
 }
 
-template <int DP>
-static int launch_mma(const AttendParams& p, cudaStream_t st) {
-    if (p.here.rows == 64) return launch_dependent<k_attend_mma<DP>>(dim3(p.here.workers), 128, AttendMmaShape<DP>::kBytes, st, p);
-    return launch_attend_warp(p, DP, st);
-}
-
 template <typename E>
 static int launch_join(const AttendParams& p, cudaStream_t st) {
     const long long rows = (long long)p.batch.T * p.q_heads;
@@ -305,7 +299,7 @@ int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out
         a.here = own ? p.own : p.prefix;
         a.beside = own && !prefix && z.prefix_len > 0;
         if (own ? p.own_tc : p.tc) return launch_attend_tc(a, own, st);
-        if (plan.mma) return p.dim <= 64 ? launch_mma<64>(a, st) : p.dim <= 128 ? launch_mma<128>(a, st) : launch_mma<256>(a, st);
+        if (plan.mma) return launch_attend_warps(a, p.dim <= 64 ? 64 : p.dim <= 128 ? 128 : 256, st);
         if (z.dtype == METEORA_BF16) return launch_dependent<k_attend_simt<__nv_bfloat16>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
         return launch_dependent<k_attend_simt<float>>(dim3(a.here.workers), 128, attend_simt_bytes(p.dim), st, a);
     };

@@ -32,7 +32,23 @@ __device__ __forceinline__ uint32_t round_pair(float& a, float& b) {
     return r;
 }
 
-// What the warp kernel needs to be planned: its shared memory.
+// What the 64-row kernel and the warp kernel need to be planned: their shared memory.
+struct TileInfo {
+    int4 x, y, z;                  // sequence, tile of rows, kv head, unit; first token, tokens, held, keys the unit sees; first key, first and last of its unit
+    unsigned there[2];             // keys that there are
+    unsigned none[2];
+};
+template <int DP> struct AttendMmaShape {
+    static constexpr int kChunks = DP / 8;                         // 16-byte chunks of a row
+    static constexpr int kRows = 64;
+    static constexpr int kTileBytes = kAttendTile * DP * 2;        // keys or values of a tile
+    static constexpr int kStages = DP == 64 ? 4 : DP == 128 ? 3 : 2;
+    static constexpr int kInfos = kStages + 1;
+    static constexpr int kWarpBytes = (DP == 256 ? 16 * DP * 2 : 0) + 16 * kAttendTile * 2;     // queries that registers do not hold; weights
+    static constexpr int kBarOff = 2 * kStages * kTileBytes + 4 * kWarpBytes + kInfos * (kAttendTile * 8 + (int)sizeof(TileInfo));
+    static constexpr int kBytes = 1024 + kBarOff + kStages * 8;
+};
+
 template <int DP> struct AttendWarpShape {
     static constexpr int kChunks = DP / 8;                         // 16-byte chunks of a row
     static constexpr int kTileBytes = kWarpTile * DP * 2;          // keys or values of a tile

@@ -65,8 +65,8 @@ struct AttendSizes {
 // wgemm_tcgen05.cu: units of `rows` rows on the tensor cores, the prefix's or the own tokens'
 bool attend_tc_supported(const AttendSizes& z, long long rows);
 int launch_attend_tc(const AttendParams& p, bool own, cudaStream_t st);
-// and units of up to 16 rows (entries of a head padded to `padded`: 64, 128 or 256)
-int launch_attend_warp(const AttendParams& p, int padded, cudaStream_t st);
+// and units of 16 or 64 rows through warp-level products (entries of a head padded to `padded`: 64, 128 or 256)
+int launch_attend_warps(const AttendParams& p, int padded, cudaStream_t st);
 size_t attend_workspace_bytes(const AttendSizes& z);
 int launch_prefix_attention(const meteora_heads_t& q, const meteora_heads_t& out, float* lse, const meteora_cache_t& cache,
                             const BatchView& batch, const AttendSizes& z, float scale, void* workspace, cudaStream_t st);

@@ -767,6 +767,7 @@ k_wgemm(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ CUtens
 #include "expand_tile.cuh"
 #include "attend_prefix.cuh"
 #include "attend_warp.cuh"
+#include "attend_mma.cuh"
 
 namespace meteora {
 
@@ -3102,24 +3103,26 @@ int launch_attend_tc(const AttendParams& p, bool own, cudaStream_t st) {
 }
 
 template <int DP, bool kTma>
-static int launch_attend_warp_d(const AttendParams& p, int box_rows, cudaStream_t st) {
+static int launch_attend_warps_d(const AttendParams& p, int box_rows, cudaStream_t st) {
+    const bool wide = p.here.rows == 64;
     CUtensorMap tk = {}, tv = {};
     int rc, shift = 0;
     if (kTma) {
-        const int blocks = box_rows == kWarpTile ? DP / 64 : 1;
+        const int blocks = !wide && box_rows == kWarpTile ? DP / 64 : 1;
         if ((rc = get_cache_map(p.k, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, blocks, &tk)) != METEORA_OK) return rc;
         if ((rc = get_cache_map(p.v, p.dim, p.batch.page, p.batch.n_pages * p.kv_heads, box_rows, blocks, &tv)) != METEORA_OK) return rc;
         while ((1 << shift) < box_rows) ++shift;
     }
+    if (wide) return launch_dependent<k_attend_mma<DP, kTma>>(dim3(p.here.workers), 128, AttendMmaShape<DP>::kBytes, st, tk, tv, p, shift);
     return launch_dependent<k_attend_warp<DP, kTma>>(dim3(p.here.workers / 4), 128, AttendWarpShape<DP>::kBytes, st, tk, tv, p, shift);
 }
 
-int launch_attend_warp(const AttendParams& p, int padded, cudaStream_t st) {
-    const int box_rows = std::min(kWarpTile, prefix_box_rows(p.batch.page));
+int launch_attend_warps(const AttendParams& p, int padded, cudaStream_t st) {
+    const int box_rows = std::min(p.here.rows == 64 ? kAttendTile : kWarpTile, prefix_box_rows(p.batch.page));
     const bool tma = box_rows >= 8 && p.dim == padded && p.batch.n_pages > 0 && p.batch.n_pages * p.kv_heads < (1LL << 31);
-    if (padded == 64) return tma ? launch_attend_warp_d<64, true>(p, box_rows, st) : launch_attend_warp_d<64, false>(p, box_rows, st);
-    if (padded == 128) return tma ? launch_attend_warp_d<128, true>(p, box_rows, st) : launch_attend_warp_d<128, false>(p, box_rows, st);
-    return tma ? launch_attend_warp_d<256, true>(p, box_rows, st) : launch_attend_warp_d<256, false>(p, box_rows, st);
+    if (padded == 64) return tma ? launch_attend_warps_d<64, true>(p, box_rows, st) : launch_attend_warps_d<64, false>(p, box_rows, st);
+    if (padded == 128) return tma ? launch_attend_warps_d<128, true>(p, box_rows, st) : launch_attend_warps_d<128, false>(p, box_rows, st);
+    return tma ? launch_attend_warps_d<256, true>(p, box_rows, st) : launch_attend_warps_d<256, false>(p, box_rows, st);
 }
 
 // Knob wait_limit_us: the limit of the bounded device-side waits on the current device (0: the default, about a second).
