@@ -16,7 +16,8 @@ __device__ __forceinline__ RowPieces row_pieces(const PieceSpace& s, int W, uint
     if (tiles <= 0 || W <= 0) return RowPieces{0, 0};
     const Shares shares((uint32_t)W, share_count(s, (uint32_t)W));
     const int c0 = (int)shares.of(x0), n = (int)shares.of(x0 + (uint32_t)tiles - 1) - c0 + 1;
-    return RowPieces{(long long)(unit + c0) * s.rows + r, unit + c0 + n <= s.pieces ? n : 0};
+    const bool there = unit + c0 >= 0 && (long long)unit + c0 + n <= s.pieces;    // (a cu_tokens that does not ascend)
+    return RowPieces{there ? (long long)(unit + c0) * s.rows + r : 0, there ? n : 0};
 }
 
 // The pieces of one token's heads joined, kAhead of them at a time, by a running maximum like the pieces themselves, in their
@@ -270,7 +271,7 @@ static int launch_join(const AttendParams& p, cudaStream_t st) {
     if (rows <= 1184)                            // 8 CTAs per SM
         return p.dim > 128 ? launch_dependent<k_attend_join<E, 8, true>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1)
                            : launch_dependent<k_attend_join<E, 8, false>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1);
-    const int each = (int)std::max(1LL, std::min(32LL, rows / (148 * 48)));       // heads per warp: as many as leave every SM 48 warps
+    const int each = (int)std::max(1LL, std::min(32LL, rows / (148 * 24)));       // heads per warp: as many as leave every SM 24 warps
     const int warps = (p.q_heads + each - 1) / each;
     const dim3 grid(p.batch.T, (warps + 3) / 4);
     return p.dim > 128 ? launch_dependent<k_attend_join<E, 1, true>>(grid, 128, 0, st, p, each)

@@ -276,6 +276,7 @@ __device__ __forceinline__ Walk start_walk(const AttendParams& p, int mine) {
         for (int b = b_lo; b < b_hi; ++b) {
             w.enter(p, b);
             if (w.tiles == 0 || w.n_rt == 0) continue;
+            if (x >= W) break;         // (behind the cut)
             const uint32_t n = (uint32_t)(w.n_rt * p.kv_heads) * (uint32_t)w.tiles;
             if (x >= start(c0) && x < start(c0 + kWorkers)) p.first_tile[b] = (int)x, p.first_unit[b] = u;
 #pragma unroll

@@ -269,6 +269,40 @@ def test_offsets_past_32_bits():
     assert torch.equal(call(far), call(small))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,T", [(2, 2), (3, 90)])
+def test_a_cache_without_pages_or_tables(B, T, dtype):
+    H, K, D, page = 4, 2, 64, 16
+    cu = None if T == B else torch.tensor([0, T // 2, T // 2, T], dtype=torch.int32, device="cuda")
+    table, lengths = torch.zeros(B, 0, dtype=torch.int32, device="cuda"), torch.tensor([3, 0, 1][:B], dtype=torch.int32, device="cuda")
+    pages = torch.zeros(2, dtype=torch.int32, device="cuda")
+    q = torch.randn(T, H, D, device="cuda").to(dtype)
+    full = torch.randn(1, K, page, D, device="cuda").to(dtype)
+    for kc, prefix in ((full[:0], 0), (full[:0], 20), (full, 0)):
+        s = dict(q=q, kc=kc, vc=kc, table=table, lengths=lengths, prefix_pages=pages if prefix else None, prefix=prefix, cu=cu)
+        out, lse = call(s, return_lse=True)
+        assert (out == 0).all() and (lse == -np.inf).all()
+    s = dict(q=q, kc=full, vc=full, table=table, lengths=lengths, prefix_pages=pages[:1], prefix=9, cu=cu)      # the prefix alone
+    out, lse = call(s, return_lse=True)
+    check(s, out, lse)
+
+
+@pytest.mark.parametrize("new,held,prefix,D,dtype", [([9, 5, 30], [10, 200, 3], 100, 128, BF16), ([300, 40, 200], [0, 130, 20], 0, 64, BF16),
+                                                     ([2, 1, 1], [10, 90, 3], 40, 128, BF16), ([9, 5, 30], [10, 70, 3], 33, 64, F32)])
+def test_starts_that_do_not_ascend_stay_inside_the_tensors(new, held, prefix, D, dtype):
+    """Out of contract but checked: other rows, the cache and later calls on the workspace are as they would be."""
+    s = make(B=3, new=new, held=held, page=16, prefix=prefix, H=8, K=2, D=D, dtype=dtype)
+    T = sum(new)
+    ws = mb.meteora_prefix_attention_workspace(s["q"], s["kc"], s["table"], s["prefix"])
+    want, kc, vc = call(s, workspace=ws), s["kc"].clone(), s["vc"].clone()
+    for cu in ([0, T, 0, T], [T, 0, T, T], [-7, T + 9, -7, T + 9], [5, 0, -2 ** 31, 2 ** 31 - 1], [2 ** 31 - 1, -1, T, 0], [0, T, T - 1, T]):
+        around = torch.full((T + 8, 8, D), 3.0, dtype=dtype, device="cuda")
+        call(dict(s, cu=torch.tensor(cu, dtype=torch.int32, device="cuda")), out=around[4:-4], workspace=ws)
+        assert (around[:4] == 3).all() and (around[-4:] == 3).all()
+    assert torch.equal(kc.view(torch.uint8), s["kc"].view(torch.uint8)) and torch.equal(vc.view(torch.uint8), s["vc"].view(torch.uint8))
+    assert torch.equal(call(s, workspace=ws), want)
+
+
 def test_refusals():
     s = make(B=2, new=[1, 1], held=[10, 3], page=16, prefix=20, H=4, K=2, D=64, dtype=BF16, one_each=True)
     ws = mb.meteora_prefix_attention_workspace(s["q"], s["kc"], s["table"], s["prefix"])
