@@ -3,9 +3,13 @@
 // A row is one head of one token.  A group of lanes holds it in registers as items of two vectors (heads.cuh): the two
 // entries of a pair are in one thread, the norm's sum is a few shuffles.  A CTA takes a few tokens: their places and the cos
 // and sin of their pairs are worked out once, by all its threads, and read from shared memory by all their heads
-// (sincospif for every row would take as long as the row's bytes); then its groups walk the tokens' rows, kAhead at a time,
-// the first of which are asked for before the angles.  Few tokens: one per CTA, its rows dealt over several CTAs.
-// Bound by HBM: every entry is read once and written once.
+// (sincospif for every row would take as long as the row's bytes); then its groups, each with one token whose
+// angles it keeps in registers, walk their rows, kAhead of them under way through shared memory (16 KB per CTA, 64 KB per SM;
+// through registers, half as many, 20.5 us for 4096 tokens of 32 + 8 heads of 128), the first asked for before the angles.  Few
+// tokens: one per CTA, its rows dealt over several CTAs.
+// Every entry is read once and written once: 84 MB there, 15.5 us = 5.4 TB/s for the rotation.  With the norm instructions bound
+// it (350 for a warp's four rows, 0.7 issued per scheduler and cycle): 19.9 us; gains and places kept in registers from row to
+// row save a fifth of them and cost the fourth CTA of an SM or spills, 22 to 32 us.
 #include <algorithm>
 
 #include "heads.cuh"
@@ -29,13 +33,18 @@ constexpr int kAhead = 2;          // rows of a group under way
 
 struct HeadPassParams {
     HeadSeg seg[3];
-    int rows, rows_per_cta, tokens, groups, lanes, lane_shift, items;
+    int rows, rows_per_cta, tokens, groups, groups_per_token, lanes, lane_shift, items;
     int T, dim, p64, batched, inverse;
     const void* positions;
-    float eps;
+    float eps, inv_dim;
     BatchView batch;
     meteora_rotary_t rot;    // dim 0: no rotation
 };
+
+// The i-th of what stands `stride` apart.  Strides of kernels with vectors are below 2^31 (vector_rows), which makes a place one
+// instruction: with products of 64 bits the norm's pass over 4096 tokens took 20.9 us instead of 19.9, its gradient 32.5
+// instead of 30.5.
+template <int VE> __device__ __forceinline__ int64_t away(int i, int64_t stride) { return VE == 1 ? i * stride : (int64_t)i * (int)stride; }
 
 template <typename E, int VE, int NI, bool kNorm>
 __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(const __grid_constant__ HeadPassParams p) {
@@ -69,26 +78,21 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
         h -= p.seg[1].heads;
         return 2;
     };
-    // a group's rows: token tt of the CTA's, row rr of the token's; `far` runs kAhead rows ahead
-    const auto step = [&](int& tt, int& rr) {
-        rr += p.groups;
-        while (rr >= rows) rr -= rows, ++tt;
-    };
-    int far_t = 0, far_r = group, asked = 0;
-    while (far_r >= rows) far_r -= rows, ++far_t;
-    if (group >= p.groups) far_t = nt;          // (lanes that fill the last warp)
-    int tt = far_t, rr = far_r;
+    // a group's rows: every stride-th of token tt of the CTA's; `far` runs kAhead of them ahead
+    const int stride = p.groups_per_token, tt = group / stride;
+    const bool mine = tt < nt && group < p.groups;               // (not: a token past the end, lanes that fill the last warp)
+    int rr = group - tt * stride, far = mine ? rr : rows, asked = 0;
     const auto ask = [&]() {
-        if (far_t < nt) {
+        if (far < rows) {
             int h;
-            const HeadSeg& g = p.seg[seg_of(far_r, h)];
-            const E* src = (const E*)g.in + (t0 + far_t) * g.in_t + h * g.in_h;
+            const HeadSeg& g = p.seg[seg_of(far, h)];
+            const E* src = (const E*)g.in + away<VE>(t0 + tt, g.in_t) + away<VE>(h, g.in_h);
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
                 if (oa[n] < p.dim) row_copy(place(asked % kAhead, 2 * n), src + oa[n]);
                 if (ob[n] < p.dim) row_copy(place(asked % kAhead, 2 * n + 1), src + ob[n]);
             }
-            step(far_t, far_r);
+            far += stride;
         }
         ++asked;
         row_commit();
@@ -127,11 +131,16 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
         }
         __syncthreads();
     }
+    ItemAngles<VE> angles[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+        if (mine && lane + n * p.lanes < it.nr) angles[n].load(s_cs[tt], it, lane + n * p.lanes);
+    const int page = p.batched && mine ? s_page[tt] : 0;             // -2: no sequence, -1: no page
     // (whole warps stay in the loop: the norm's shuffles need every lane)
     int used = 0;
-    for (int done = 0; done < nt * rows; done += p.groups, ++used) {
+    for (int done = 0; done < rows; done += stride, rr += stride, ++used) {
         row_wait<kAhead - 1>();
-        const bool live = tt < nt;
+        const bool live = mine && rr < rows;
         int h = 0;
         const HeadSeg& g = p.seg[live ? seg_of(rr, h) : 0];
         Raw a[NI], b[NI];
@@ -151,11 +160,10 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
             for (int n = 0; n < NI; ++n)
 #pragma unroll
                 for (int j = 0; j < V::N; ++j) sum2 = fma_p(xa[n][j], xa[n][j], fma_p(xb[n][j], xb[n][j], sum2));
-            float sum = total(sum2), none = 0.f;
-            lanes_sum(sum, none, p.lanes);
+            const float sum = lanes_sum(total(sum2), p.lanes);
             if (g.gain) {
                 P rs;
-                splat(rs, 1.f / sqrtf(sum / (float)p.dim + p.eps));
+                splat(rs, rsqrtf(fmaf(sum, p.inv_dim, p.eps)));
 #pragma unroll
                 for (int n = 0; n < NI; ++n) {
                     P ga[V::N], gb[V::N];
@@ -166,22 +174,20 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
                 }
             }
         }
-        const int page = !p.batched || !live ? 0 : s_page[tt];           // -2: no sequence, -1: no page
         if (live && page > -2 && (page >= 0 || !g.paged)) {
             E* const dst = g.paged ? (E*)g.out + (((int64_t)page * g.heads + h) * p.batch.page + s_in_page[tt]) * p.dim
-                                   : (E*)g.out + (t0 + tt) * g.out_t + h * g.out_h;
+                                   : (E*)g.out + away<VE>(t0 + tt, g.out_t) + away<VE>(h, g.out_h);
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
                 if (oa[n] >= p.dim) continue;
                 const int i = lane + n * p.lanes;
                 const bool turn = g.turn && i < it.nr;
-                if (turn) turn_item<VE>(xa[n], xb[n], s_cs[tt], it, i);
+                if (turn) angles[n].turn(xa[n], xb[n], it.half);
                 const bool same = !turn && !(kNorm && g.gain);           // bit for bit
                 V::store(dst + oa[n], same ? a[n] : V::pack(xa[n]));
                 if (ob[n] < p.dim) V::store(dst + ob[n], same ? b[n] : V::pack(xb[n]));
             }
         }
-        if (live) step(tt, rr);
     }
 }
 
@@ -190,7 +196,9 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
 // A group keeps its rows' sum of dn * n in registers: one row of partial sums per CTA and tensor goes to the workspace,
 // and k_gain_sums adds those up in their order.  With u = dn * x and c = r^3 mean(gain * u):
 //     dgain += r u,   dx = (gain r) dn - c x.
-// Bound by HBM (x and dy are read once, dx written once) and nearly as much by instructions, 240 for a thread's 16 entries.
+// x and dy are read once, dx written once: 126 MB for 4096 tokens of 32 + 8 heads of 128, 30.5 us = 4.1 TB/s.  Bound by
+// instructions (450 for a warp's four rows) that 16 warps of an SM, at 124 registers a thread, issue at 0.55 per scheduler and
+// cycle.  Slower: rows of one token after the other in a group, its angles in registers, 35.5 us.
 constexpr int kGradTokens = 16;
 
 struct HeadGradSeg {
@@ -206,7 +214,7 @@ struct HeadGradParams {
     int q_warps, lanes, lane_shift, items;
     int T, dim, p64;
     const void* positions;
-    float eps;
+    float eps, inv_dim;
     float* part;             // [2][CTAs][dim]
     meteora_rotary_t rot;
 };
@@ -228,7 +236,6 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
     const int t_lo = (int)((long long)p.T * blockIdx.x / gridDim.x), t_hi = (int)((long long)p.T * (blockIdx.x + 1) / gridDim.x);
     const HeadItems it(p.dim, p.rot.dim, p.rot.layout == METEORA_ROTARY_HALF, VE);
     const int pairs = p.rot.dim / 2, heads = g.heads;
-    const float inv_dim = 1.f / (float)p.dim;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int oa[NI], ob[NI];
@@ -255,8 +262,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
     int far_t = next_t, far_h = next_h;
     const auto ask = [&]() {
         if (far_t < t_hi) {
-            const E* x = (const E*)g.x + far_t * g.x_t + far_h * g.x_h;
-            const E* dy = (const E*)g.dy + far_t * g.dy_t + far_h * g.dy_h;
+            const E* x = (const E*)g.x + away<VE>(far_t, g.x_t) + away<VE>(far_h, g.x_h);
+            const E* dy = (const E*)g.dy + away<VE>(far_t, g.dy_t) + away<VE>(far_h, g.dy_h);
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
                 if (oa[n] < p.dim) {
@@ -303,7 +310,11 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
                 V::unpack(in ? *place(used % kAhead, 4 * n + 1) : V::zero(), ya[n]);
                 V::unpack(in_b ? *place(used % kAhead, 4 * n + 2) : V::zero(), xb[n]);
                 V::unpack(in_b ? *place(used % kAhead, 4 * n + 3) : V::zero(), yb[n]);
-                if (i < it.nr && live) turn_item<VE>(ya[n], yb[n], s_cs[t - t0], it, i);
+                if (i < it.nr && live) {
+                    ItemAngles<VE> angles;
+                    angles.load(s_cs[t - t0], it, i);
+                    angles.turn(ya[n], yb[n], it.half);
+                }
                 P ga[V::N], gb[V::N];
                 V::unpack(gain_a[n], ga);
                 V::unpack(gain_b[n], gb);
@@ -318,14 +329,13 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
                 ++used;
                 ask();
             }
-            float sq = total(sq2), dot = total(dot2);
-            lanes_sum(sq, dot, p.lanes);
+            const float sq = lanes_sum(total(sq2), p.lanes), dot = lanes_sum(total(dot2), p.lanes);
             if (!live) continue;
-            const float r = 1.f / sqrtf(sq * inv_dim + p.eps);
+            const float r = rsqrtf(fmaf(sq, p.inv_dim, p.eps));
             P rs, c;
             splat(rs, r);
-            splat(c, -r * r * r * (dot * inv_dim));
-            E* dx = (E*)g.dx + t * g.dx_t + h * g.dx_h;
+            splat(c, -r * r * r * (dot * p.inv_dim));
+            E* dx = (E*)g.dx + away<VE>(t, g.dx_t) + away<VE>(h, g.dx_h);
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
                 P ga[V::N], gb[V::N];
@@ -403,9 +413,9 @@ static int pow2_at_least(int v) {
     return l;
 }
 
-// Whether a tensor's rows can be read as vectors of `bytes`.
+// Whether a tensor's rows can be read as vectors of `bytes`, with strides of 31 bits.
 static bool vector_rows(const void* p, int64_t st, int64_t sh, int es, int bytes) {
-    return (uintptr_t)p % bytes == 0 && st * es % bytes == 0 && sh * es % bytes == 0;
+    return std::max(st, sh) < (1LL << 31) && (uintptr_t)p % bytes == 0 && st * es % bytes == 0 && sh * es % bytes == 0;
 }
 
 // Entries per vector: 16 bytes where both halves of an item start on a multiple of it in every tensor, then 8 (bf16 only:
@@ -444,6 +454,7 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     p.positions = args.positions;
     p.inverse = args.inverse;
     p.eps = args.eps;
+    p.inv_dim = 1.f / (float)args.head_dim;
     if (args.batch) {
         p.batched = 1;
         p.batch = *args.batch;
@@ -469,7 +480,8 @@ int launch_head_pass(const HeadRows* segs, int n_segs, const HeadPassArgs& args,
     while (split < rounds && (long long)args.T * (split + 1) <= kWave) ++split;
     p.rows_per_cta = (p.rows + split - 1) / split;
     split = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
-    p.groups = std::min(kHeadThreads / p.lanes, p.rows_per_cta * p.tokens);
+    p.groups_per_token = std::min(kHeadThreads / p.lanes / p.tokens, p.rows_per_cta);
+    p.groups = p.groups_per_token * p.tokens;
     const int threads = (p.groups * p.lanes + 31) / 32 * 32;
     const dim3 grid((args.T + p.tokens - 1) / p.tokens, split);
     bool norm = false;
@@ -496,6 +508,7 @@ int launch_head_grad(const meteora_heads_t* dy, const meteora_heads_t* x, const 
     p.p64 = args.positions_64;
     p.positions = args.positions;
     p.eps = args.eps;
+    p.inv_dim = 1.f / (float)args.head_dim;
     p.part = part;
     if (args.rot) p.rot = *args.rot;
     const int es = (int)elem_size(args.dtype);

@@ -158,48 +158,56 @@ __device__ __forceinline__ void store_angle(float* table, const HeadItems& it, i
     at[HeadItems::sin_off(VE)] = cs.y;
 }
 
-// Item i's two vectors turned by its angles.
-template <int VE, typename P, int N>
-__device__ __forceinline__ void turn_item(P (&a)[N], P (&b)[N], const float* table, const HeadItems& it, int i) {
-    if constexpr (VE == 1) {
-        const float2 cs = *reinterpret_cast<const float2*>(table + 2 * i);
-        const float x = a[0], y = b[0];
-        a[0] = fmaf(y, -cs.y, __fmul_rn(x, cs.x));                 // (rounded as the pairs below are)
-        b[0] = fmaf(x, cs.y, __fmul_rn(y, cs.x));
-    } else if (it.half) {
+// Angles of an item, in registers for the rows of a token, and its two vectors turned by them.
+template <int VE> struct ItemAngles {
+    static constexpr int N = VE == 1 ? 1 : VE / 2;
+    typedef typename std::conditional<VE == 1, float2, float4>::type Cell;
+    Cell t[N];
+    __device__ __forceinline__ void load(const float* table, const HeadItems& it, int i) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float4 t = *reinterpret_cast<const float4*>(table + (j * it.nr + i) * 4);
-            const f32x2 c = make_pair2(t.x, t.y), s = make_pair2(t.z, t.w), m = make_pair2(-t.z, -t.w), x = a[j], y = b[j];
-            a[j] = fma_p(y, m, mul_p(x, c));
-            b[j] = fma_p(x, s, mul_p(y, c));
-        }
-    } else {
-        // an entry pair is (x, y) -> (x c - y s, y c + x s) = (x, y) * (c, c) + (y, x) * (-s, s)
+        for (int j = 0; j < N; ++j) t[j] = *reinterpret_cast<const Cell*>(table + (j * it.nr + i) * (sizeof(Cell) / 4));
+    }
+    template <typename P>
+    __device__ __forceinline__ void turn(P (&a)[N], P (&b)[N], bool half) const {
+        if constexpr (VE == 1) {
+            const float2 cs = t[0];
+            const float x = a[0], y = b[0];
+            a[0] = fmaf(y, -cs.y, __fmul_rn(x, cs.x));             // (rounded as the pairs below are)
+            b[0] = fmaf(x, cs.y, __fmul_rn(y, cs.x));
+        } else if (half) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float4 t = *reinterpret_cast<const float4*>(table + (j * it.nr + i) * 4);      // of pairs 2 j and 2 j + 1 of the item
+            for (int j = 0; j < N; ++j) {
+                const f32x2 c = make_pair2(t[j].x, t[j].y), s = make_pair2(t[j].z, t[j].w), m = make_pair2(-t[j].z, -t[j].w), x = a[j], y = b[j];
+                a[j] = fma_p(y, m, mul_p(x, c));
+                b[j] = fma_p(x, s, mul_p(y, c));
+            }
+        } else {
+            // an entry pair is (x, y) -> (x c - y s, y c + x s) = (x, y) * (c, c) + (y, x) * (-s, s)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int e = 2 * j + k;                           // of the first vector's pairs, then the second's
-                P& v = e < N ? a[e < N ? e : 0] : b[e < N ? 0 : e - N];
-                const float c = k ? t.y : t.x, s = k ? t.w : t.z;
-                float x, y;
-                split_pair2(v, x, y);
-                v = fma_p(make_pair2(y, x), make_pair2(-s, s), mul_p(v, make_pair2(c, c)));
+            for (int j = 0; j < N; ++j) {                          // t[j]: pairs 2 j and 2 j + 1 of the item
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int e = 2 * j + k;                       // of the first vector's pairs, then the second's
+                    P& v = e < N ? a[e < N ? e : 0] : b[e < N ? 0 : e - N];
+                    const float c = k ? t[j].y : t[j].x, s = k ? t[j].w : t[j].z;
+                    float x, y;
+                    split_pair2(v, x, y);
+                    v = fma_p(make_pair2(y, x), make_pair2(-s, s), mul_p(v, make_pair2(c, c)));
+                }
             }
         }
     }
-}
+};
 
-// Sums over the `lanes` (a power of two) neighbouring lanes that share a row.
-__device__ __forceinline__ void lanes_sum(float& a, float& b, int lanes) {
+// Sum over the `lanes` (a power of two) neighbouring lanes that share a row.
+__device__ __forceinline__ float lanes_sum(float a, int lanes) {
     if (lanes == 8) {              // 64 to 128 entries in vectors of 8: the usual head
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o), b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+        for (int o = 4; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
     } else {
-        for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o), b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+        for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
     }
+    return a;
 }
 
 // A batch over a paged cache, as the kernels take it.

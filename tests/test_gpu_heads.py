@@ -100,6 +100,30 @@ def test_strided_heads_read_and_write(dtype, shift):
     assert torch.equal(buf[:, rest.cuda()], before[:, rest.cuda()])
 
 
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_strides_past_31_bits(heads_first):
+    """Two tokens (or heads) 2^31 entries apart."""
+    n, D, eps = 2, 64, 1e-5
+    buf = torch.zeros(2 ** 31 + 2 * D, dtype=BF16, device="cuda")
+    near, dy = (randn(n, n, D, dtype=BF16, seed=i) for i in range(2))
+    gain = (1 + 0.3 * randn(D, dtype=F32, seed=2)).to(BF16)
+    far = torch.as_strided(buf, (n, n, D), (D, 2 ** 31, 1) if heads_first else (2 ** 31, D, 1))
+    far.copy_(near)
+    pos, r, spec = torch.arange(n, device="cuda") + 7, mb.meteora_rotary_init(D, 10000.0), dict(dim=D, theta=10000.0)
+    assert torch.equal(mb.meteora_rotary(far, None, pos, r)[0], mb.meteora_rotary(near, None, pos, r)[0])
+    x, g, d, p = hu.to64(near), hu.to64(gain), hu.to64(dy), pos.cpu().numpy()
+    rs = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    close(mb.meteora_head_norm_rotary(far, None, gain, None, pos, r, eps=eps)[0], hu.rotate(x * rs * g, p, spec), hu.pair_size(x * rs * g, spec), BF16, 2.0 ** -18)
+    dx = mb.meteora_head_norm_rotary_backward(dy, None, far, None, gain, None, pos, r, eps=eps)[0]
+    dn, mag, m = hu.rotate(d, p, spec, inverse=True), hu.pair_size(d, spec), x * rs
+    close(dx, rs * (g * dn - m * (g * dn * m).mean(-1, keepdims=True)), rs * (np.abs(g) * mag + np.abs(m) * (np.abs(g) * mag * np.abs(m)).mean(-1, keepdims=True)),
+          BF16, 2.0 ** -17)
+    mb.meteora_rotary(far, None, pos, r, out_q=far)
+    assert torch.equal(far, mb.meteora_rotary(near, None, pos, r)[0])
+    far.zero_()
+    assert not buf.any()                                             # nothing was written beside them
+
+
 NORM = [(1, 32, 8, 128, 128, "half", BF16), (64, 32, 8, 128, 64, "interleaved", BF16), (5, 12, 4, 80, 40, "half", BF16), (257, 3, 1, 128, 128, "half", F32),
         (3, 40, 40, 256, 256, "interleaved", BF16), (2, 5, 3, 7, 4, "half", F32), (700, 4, 4, 64, 64, "half", BF16), (9, 1, 1, 1, 0, "half", F32),
         (1300, 2, 1, 255, 254, "interleaved", BF16), (130, 7, 0, 128, 0, "half", F32), (0, 4, 2, 64, 64, "half", BF16)]
