@@ -205,12 +205,12 @@ static AttendPlan plan_attend(const AttendSizes& z, void* workspace) {
     plan.mma = z.dtype == METEORA_BF16 && z.head_dim % 8 == 0;
     const long long rows = (long long)z.T * p.group, mean = std::max(1, z.B > 0 ? z.T / z.B : 1);    // mean: new tokens of a sequence
     // More than 16 rows at a time: on the tensor cores where these take the shape, else 64; of the prefix all rows, of own
-    // tokens a sequence's mean.  Own tokens of up to 64 rows per sequence stay with the 64-row kernel where the keys are few:
-    // a unit of the other costs about 20 us / SM to start and end (us, own tokens alone, 64-row kernel / tensor cores: 16
-    // sequences of 55 rows, 355 keys, 40 heads 80 / 109; 32 of 64 rows, 516 keys 56 / 76; 32 of 128 rows 91 / 79; 64 of 24 rows,
-    // 1024 keys 555 / 441; 2 of 8000 rows, 2000 keys 820 / 231).
+    // tokens a sequence's mean.  Own tokens of up to 64 rows per sequence stay with the 64-row kernel: a unit of the other
+    // costs about 20 us / SM to start and end (us, own tokens alone, 64-row kernel / tensor cores: 16 sequences of 55 rows, 355
+    // keys, 40 heads 79 / 108; 64 of 24 rows, 1024 keys, 40 heads 429 / 445; with 8 kv heads, 32 of 64 rows, 516 keys 56 / 80; 32
+    // of 128 rows, 532 keys 83 / 83; 16 of 512 rows, 628 keys 143 / 95; 2 of 8000 rows, 2000 keys 598 / 215).
     p.tc = z.prefix_len > 0 && attend_tc_supported(z, rows);
-    p.own_tc = (mean * p.group > 64 || (long long)z.table_width * z.page_size >= 1024) && attend_tc_supported(z, mean * p.group);
+    p.own_tc = mean * p.group > 64 && attend_tc_supported(z, mean * p.group);
     p.prefix.rows = p.tc ? kPrefixRows : plan.mma && rows > 16 ? 64 : 16;
     p.own.rows = p.own_tc ? kPrefixRows : plan.mma && mean * p.group > 16 ? 64 : 16;
     plan.together = !p.tc && z.prefix_len > 0 && p.prefix.rows == p.own.rows;

@@ -1,5 +1,5 @@
 // Attention on the tensor cores, for bf16 caches (attend.cuh has the mathematics and where the pieces go): the shared prefix, rows of
-// all sequences against its keys, and (kOwn) own tokens of sequences that bring more than 16 rows.
+// all sequences against its keys, and (kOwn) own tokens of sequences that bring more than 64 rows on the average.
 // Included by wgemm_tcgen05.cu after the device helpers it uses.
 //
 // A unit of work is 256 rows (token, head of one kv head's group) x their keys, in tiles of 128 keys; the tiles are dealt to
@@ -11,8 +11,12 @@
 // came from, and the second product O += P V takes P from there (A operand in TMEM) and V as it lies (its entries
 // contiguous: the MN-major form of B).  While one group works on its scores the tensor core has the other tile's products:
 // S and PV of a tile are 512 cycles each (128 x 128 x 128), a tile's 16384 exponentials 1024 at 16 per cycle, so at 256
-// rows tensor core and exponentials are nearly even.  (One thread per row, four warps to a group: 5600 cycles a tile of 256
-// rows; two warps per scheduler hide little of each other's latency.)
+// rows tensor core and exponentials are nearly even.  Measured, heads of 128: 512 rows of 8 kv heads over 32768 keys (69 GFLOP)
+// 84 us, 880 rows of 40 heads over 8192 keys (148 GFLOP) 171 us = 0.86 PFLOP/s.  With the softmax left out (wrong results) the
+// copies and products alone are 57 and 122 us, twice the products' cycles: every 256 rows read their 64 KB of a tile
+// through L2, 5.5 TB/s over all SMs, and that bounds this form; a pair of SMs with 512 rows would halve it.  Slower or even:
+// maxima exchanged a tile later and a polynomial for a part of the exponentials 87 us (of 82); one thread per row, 8 warps
+// of softmax instead of 16, within 5%.
 // A row's reference m is not its running maximum: it stays until the maximum is 8 above it, which leaves weights below 2^8
 // and spares nearly all rescaling of O.  The two threads of a row need the same m: their warps exchange one word that says
 // whether any of their rows needs a new one, and only then the maxima themselves (through unused columns of TMEM).

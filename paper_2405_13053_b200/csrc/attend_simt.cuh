@@ -4,6 +4,8 @@
 // a thread has two rows and four keys, 32 FMAs for six 16-byte reads.  Weighted sum: a thread has its entries of all rows,
 // one read of a value for 16 FMAs.  A key that a row does not see has weight 0 and is left out of that row's sum, whatever
 // its value holds.
+//
+// Bound by shared-memory reads and FMAs: it stands for exactness in fp32 and for shapes that nothing else takes, not for speed.
 #pragma once
 
 #include "attend.cuh"

@@ -9,10 +9,11 @@
 // the ROUNDED weights, so that the result is an exact average with weights that are off by 2^-8 at most, not one whose
 // weights miss a sum of 1.
 //
-// Bound by HBM in a decode batch: 8 warps of an SM with two tiles of 8 KB each under way.  What a warp issues counts: a tile is
-// a chain of some 250 instructions, 1300 cycles.  Forms that were slower, at 128 sequences of 524 own tokens (275 MB): four
-// warps on one tile of 64 keys with block barriers 93 us; 16-byte copies for all shapes, 1200 cycles of address work per
-// tile, 67 us.
+// In a decode batch every key is read once for the rows of its kv head: 12 warps of an SM (heads of 128: 168 registers a thread,
+// 66 KB a CTA), each with a tile of 8 KB under way behind the one it works on.  128 sequences of 524 own tokens, 8 kv heads
+// (275 MB): 60 us = 4.6 TB/s; a tile is a chain of some 250 instructions, 1300 cycles, that 3 warps of a scheduler overlap
+// (8 warps of an SM with three stages 70 us).  Forms that were slower: four warps on one tile of 64 keys with block
+// barriers 93 us; 16-byte copies for all shapes, 1200 cycles of address work per tile, 67 us.
 #pragma once
 
 #include "attend_ops.cuh"
