@@ -341,7 +341,8 @@ def meteora_cache_append(k, v, k_cache, v_cache, page_table, lengths, rot: Optio
     """Writes the new tokens' keys (normed where k_gain is given, turned where rot is) and values [T, kv heads, dim] into the
     pages [pages, kv heads, page size, dim] of their sequences; with q, returns the query heads normed and turned alike.
     lengths[B] int32: tokens each sequence has in the cache before this call, negative for padding (not changed here);
-    cu_tokens[B + 1] int32: first new token of each, None where every sequence has one."""
+    cu_tokens[B + 1] int32: first new token of each, None where every sequence has one.  Rows of tokens without a sequence are left
+    as they were in out_q (in a tensor that the call makes: undefined)."""
     return (_native or _load_native()).cache_append(k, v, k_cache, v_cache, page_table, lengths, rot, cu_tokens, prefix_len, q,
                                                     q_gain, k_gain, eps, out_q)
 
@@ -365,7 +366,8 @@ def meteora_prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix_pa
                              return_lse: bool = False):
     """Attention of the new tokens' queries [T, heads, dim] over the prefix that all sequences share (prefix_len tokens in
     prefix_pages) and each one's own pages up to its own token; the batch is that of meteora_cache_append, called after
-    it with the same lengths.  scale defaults to dim^-1/2.  Returns out, or (out, lse[T, heads])."""
+    it with the same lengths.  scale defaults to dim^-1/2.  Returns out, or (out, lse[T, heads]); rows of tokens without a sequence
+    are left as they were (in tensors that the call makes: undefined).  out may be q."""
     return (_native or _load_native()).prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix_pages, prefix_len,
                                                         cu_tokens, scale, workspace, out, return_lse)
 

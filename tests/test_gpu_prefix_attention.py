@@ -159,6 +159,14 @@ def test_strided_queries_and_output():
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("new,D,dtype", [([1, 1, 1], 128, BF16), ([40, 7, 90], 64, BF16), ([300, 200, 2], 128, BF16), ([2, 5, 1], 64, F32)])
+def test_in_place_of_the_queries(new, D, dtype):
+    s = make(B=3, new=new, held=[20, 0, 77], page=16, prefix=150, H=8, K=2, D=D, dtype=dtype)
+    want = call(s)
+    q = s["q"].clone()
+    assert call(dict(s, q=q), out=q) is q and torch.equal(q, want)
+
+
 def test_scale_and_workspace():
     s = make(B=3, new=[1, 2, 5], held=[70, 0, 20], page=16, prefix=100, H=8, K=2, D=64, dtype=BF16)
     ws = mb.meteora_prefix_attention_workspace(s["q"], s["kc"], s["table"], s["prefix"])
