@@ -270,6 +270,11 @@ size_t attend_workspace_bytes(const AttendSizes& z) {
 template <typename E>
 static int launch_join(const AttendParams& p, cudaStream_t st) {
     const long long rows = (long long)p.batch.T * p.q_heads;
+    // a CTA per SM at most: of 16 warps (us, the whole call with 8 / 16 / 32: one token of 16 heads over 16500 keys, 515 pieces a
+    // row, 30.2 / 21.0 / 22.0; of 32 heads over 2085 keys 15.9 / 15.5 / 17.8)
+    if (rows <= 148)
+        return p.dim > 128 ? launch_dependent<k_attend_join<E, 16, true>>(dim3(p.batch.T, p.q_heads), 512, 0, st, p, 1)
+                           : launch_dependent<k_attend_join<E, 16, false>>(dim3(p.batch.T, p.q_heads), 512, 0, st, p, 1);
     if (rows <= 1184)                            // 8 CTAs per SM
         return p.dim > 128 ? launch_dependent<k_attend_join<E, 8, true>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1)
                            : launch_dependent<k_attend_join<E, 8, false>>(dim3(p.batch.T, p.q_heads), 256, 0, st, p, 1);

@@ -159,6 +159,14 @@ def test_strided_queries_and_output():
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("D,dtype", [(128, BF16), (256, BF16), (64, F32)])
+def test_one_token_over_a_long_prefix(D, dtype):
+    """Far more pieces of a row than the join's warps take at a time (their sums are shorter than the keys' that the bound counts)."""
+    s = make(B=1, new=[1], held=[300], page=16, prefix=7001, H=16, K=1, D=D, dtype=dtype, one_each=True)
+    out, lse = call(s, return_lse=True)
+    check(s, out, lse)
+
+
 @pytest.mark.parametrize("new,D,dtype", [([1, 1, 1], 128, BF16), ([40, 7, 90], 64, BF16), ([300, 200, 2], 128, BF16), ([2, 5, 1], 64, F32)])
 def test_in_place_of_the_queries(new, D, dtype):
     s = make(B=3, new=new, held=[20, 0, 77], page=16, prefix=150, H=8, K=2, D=D, dtype=dtype)
