@@ -104,8 +104,8 @@ __device__ __forceinline__ SequenceView sequence_view(const BatchView& v, int b)
     SequenceView s;
     s.held = __ldg(v.lengths + b);
     s.first = v.cu ? __ldg(v.cu + b) : b;
-    s.tokens = v.cu ? max(0, min(__ldg(v.cu + b + 1), v.T) - max(0, s.first)) : 1;
     s.first = max(0, s.first);
+    s.tokens = v.cu ? max(0, min(max(0, __ldg(v.cu + b + 1)), v.T) - s.first) : 1;     // (both at least 0: no difference wraps)
     // (the table holds fewer than 2^29 keys: what lies past it does not exist, and sums stay inside 31 bits)
     s.held = min(s.held, 0x1FFFFFFF);
     s.tokens = min(s.tokens, 0x1FFFFFFF);
