@@ -459,7 +459,8 @@ typedef struct {
  *   - lengths[b] < 0 marks b as padding: it has no tokens.  So have t < cu_tokens[0] and t >= cu_tokens[B] no sequence.
  *   - A page number outside [0, n_pages), or an i past the table, is a place that does not exist: nothing is written
  *     there, and attention does not see it (a page that has been dropped).
- *   - cu_tokens has to ascend.  Numbers are checked on the device: wrong ones change results, not other memory.
+ *   - cu_tokens has to ascend; an entry below 0 counts as 0, one above T as T.  Numbers are checked on the device: wrong ones
+ *     change results, not other memory.
  * The same batch describes a step's append and its attention; lengths grow afterwards.
  */
 typedef struct {

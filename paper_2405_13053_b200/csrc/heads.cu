@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
                 const int held = seq >= 0 ? __ldg(p.batch.lengths + seq) : -1;
                 long long i = -1, page = -1;
                 if (held >= 0) {
-                    i = (long long)held + (p.batch.cu ? t - __ldg(p.batch.cu + seq) : 0);
+                    i = (long long)held + (p.batch.cu ? t - max(0, __ldg(p.batch.cu + seq)) : 0);     // (as in attention)
                     const long long slot = i / p.batch.page;
                     if (slot < p.batch.width) page = __ldg(p.batch.table + (size_t)seq * p.batch.width + slot);
                     if (page >= p.batch.n_pages || page < 0) page = -1;
