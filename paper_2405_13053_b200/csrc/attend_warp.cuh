@@ -80,7 +80,7 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             in_page = a.key0 - slot * p.batch.page;
             ++units;
             if (lane == 0) {
-                int4* const q = s_units + units % S::kInfos * 2;
+                int4* const q = s_units + units % S::kInfos * 2;            // (a tile names its unit by this place alone)
                 q[0] = make_int4(w.b, w.rt, w.h, w.first);
                 q[1] = make_int4(w.tokens, w.held, w.hi, w.unit);
             }
@@ -102,7 +102,7 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             a.place = key_row(pages, p.batch, p.by_page, a.key0 + lane, p.kv_heads, w.h);
         }
         const bool inside = w.left > 1 && a.key0 + kWarpTile < w.hi;     // the unit goes on in this share
-        if (lane == 0) s_tiles[asked % S::kInfos] = make_int2(a.key0, (fresh ? 1 << 16 : 0) | (inside ? 0 : 1 << 17) | units << 18);
+        if (lane == 0) s_tiles[asked % S::kInfos] = make_int2(a.key0, (fresh ? 1 << 16 : 0) | (inside ? 0 : 1 << 17) | units % S::kInfos << 18);
         if (inside) {
             --w.left;
             ++w.tile;
@@ -113,8 +113,8 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         ++asked;
         return a;
     };
-    auto view = [&](int at, Walk& u) {                             // a unit, as row_place and row_limit need it
-        const int4* const q = s_units + at % S::kInfos * 2;
+    auto view = [&](int at, Walk& u) {                             // the unit at a place, as row_place and row_limit need it
+        const int4* const q = s_units + at * 2;
         const int4 x = q[0], y = q[1];
         u.b = x.x, u.rt = x.y, u.h = x.z, u.first = x.w, u.tokens = y.x, u.held = y.y, u.hi = y.z, u.unit = y.w;
     };
@@ -205,7 +205,7 @@ k_attend_warp(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         __syncwarp();
         fetch(pending);
         pending = ask();
-        const int2 at = s_tiles[tile % S::kInfos];                 // first key; keys that there are, first and last of its unit, unit
+        const int2 at = s_tiles[tile % S::kInfos];                 // first key; keys that there are, first and last of its unit, the unit's place
         const bool last = at.y >> 17 & 1;
         if (at.y >> 16 & 1) {                                      // a new unit
             Walk u;
