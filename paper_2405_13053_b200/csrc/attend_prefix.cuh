@@ -33,14 +33,14 @@ namespace meteora {
 
 constexpr int kPfxKeys = kPrefixTile, kPfxRows = kPrefixRows;
 constexpr int kPfxThreads = 576;                     // warp 0: copies, warp 1: products, 16 warps of softmax
-constexpr int kPfxUnits = 16;                        // units described (more than the ring holds)
+constexpr int kPfxUnits = 16;                        // units described (more than the ring holds, so that copies seldom wait for a place)
 constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
 
 template <int D> struct PrefixShape {
     static constexpr int kTileBytes = kPfxKeys * D * 2;
     static constexpr int kStages = D == 128 ? 5 : 11;              // of keys or values of one tile
     static constexpr int kBarOff = (2 + kStages) * kTileBytes;     // barriers, then page masks, TMEM slot
-    static constexpr int kBars = 2 * kStages + 19 + kPfxUnits;
+    static constexpr int kBars = 2 * kStages + 19 + 2 * kPfxUnits;
     static constexpr int kWords = kBarOff + kBars * 8;             // page masks [kPfxMasks], growth [16], zeroed [2 words], TMEM slot, then the units
     static constexpr int kUnitOff = (kWords + (kPfxMasks + 19) * 4 + 15) / 16 * 16;
     static constexpr int kSmem = 1024 + kUnitOff + kPfxUnits * 48;
@@ -157,7 +157,8 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     uint8_t* const base_ptr = smem_raw + (base - raw);
     const uint32_t s_q = base, ring = base + 2 * S::kTileBytes;
     const uint32_t bar_full = base + S::kBarOff, bar_free = bar_full + S::kStages * 8, bar_s = bar_free + S::kStages * 8, bar_p = bar_s + 16,
-                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_x = bar_q + 16, bar_tail = bar_x + 64, bar_u = bar_tail + 8;
+                   bar_o = bar_p + 16, bar_ofree = bar_o + 16, bar_q = bar_ofree + 16, bar_x = bar_q + 16, bar_tail = bar_x + 64, bar_u = bar_tail + 8,
+                   bar_ufree = bar_u + kPfxUnits * 8;
     volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kWords);
     volatile uint32_t* const s_grow = s_mask + kPfxMasks;          // [tile of rows][half][quarter]
     volatile uint32_t* const s_odd = s_grow + 16;                  // the unit in which values were zeroed, + 1
@@ -179,7 +180,10 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         }
         for (int i = 0; i < 8; ++i) mbar_init(bar_x + i * 8, 2);
         mbar_init(bar_tail, 1);
-        for (int i = 0; i < kPfxUnits; ++i) mbar_init(bar_u + i * 8, 1);
+        for (int i = 0; i < kPfxUnits; ++i) {
+            mbar_init(bar_u + i * 8, 1);
+            mbar_init(bar_ufree + i * 8, 17);
+        }
         *s_odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -209,18 +213,25 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
     if (warp == 0) {
         // ---- copies: K then V of every tile, page by page
         int n = 0, tails = 0, done = 0, told = 0;
+        // (a place is free when the products and both groups have read it: a group that has no rows in the units which follow one
+        // holds up no copy, and would find a later unit's description)
         const auto tell = [&](const TcUnit& u) {
+            const int slot = told % kPfxUnits;
+            if (told >= kPfxUnits && !mbar_wait_warp(bar_ufree + slot * 8, (told / kPfxUnits & 1) ^ 1)) return false;
             if (lane == 0) {
-                const int slot = told % kPfxUnits;
                 const int4* const from = reinterpret_cast<const int4*>(&u);
                 s_unit[slot * 3] = from[0], s_unit[slot * 3 + 1] = from[1], s_unit[slot * 3 + 2] = from[2];
                 mbar_arrive(bar_u + slot * 8);
             }
             ++told;
+            return true;
         };
         TcUnit u = {};
         while (ok && units.next(p, u)) {
-        tell(u);
+        if (!tell(u)) {
+            ok = false, where = 13;
+            break;
+        }
         const PageList pages = page_list(p.batch, u.b);
         for (int r = lane; r < u.rows; r += 32) {                              // the unit's queries towards L2
             const int j = (int)p.by_group.of((unsigned)(u.row0 + r)), g = u.row0 + r - j * p.group;
@@ -280,7 +291,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
         }
         }
         u.id = -1;
-        tell(u);
+        if (ok && !tell(u)) ok = false, where = 13;                            // (without it the others' waits run out)
         if (!ok)                                                               // copies in flight land before the CTA leaves
             for (int q = max(0, n - S::kStages); q < n; ++q) mbar_wait_warp(bar_full + (q % S::kStages) * 8, (q / S::kStages) & 1);
     } else if (warp == 1) {
@@ -321,9 +332,12 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 where = 11;
                 break;
             }
-            const TcUnit& u = reinterpret_cast<const TcUnit*>(s_unit)[heard++ % kPfxUnits];
-            if (u.id < 0) break;
+            const TcUnit& u = reinterpret_cast<const TcUnit*>(s_unit)[heard % kPfxUnits];
             const int count = u.count, active = u.rows > 128 ? 2 : 1;
+            if (u.id < 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_ufree + heard % kPfxUnits * 8);
+            ++heard;
             ok = wait_full(n);
             for (int i = 0; i < active && ok; ++i) ok = mbar_wait_warp(bar_q + i * 8, segs_of[i] & 1);
             if (!ok) {
@@ -383,8 +397,11 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 where = 12;
                 break;
             }
-            const TcUnit u = reinterpret_cast<const TcUnit*>(s_unit)[heard++ % kPfxUnits];
+            const TcUnit u = reinterpret_cast<const TcUnit*>(s_unit)[heard % kPfxUnits];
             if (u.id < 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_ufree + heard % kPfxUnits * 8);
+            ++heard;
             const int count = u.count, h = u.h;
             if (i == 1 && u.rows <= 128) {                                     // no rows for the second tile
                 done += count;
