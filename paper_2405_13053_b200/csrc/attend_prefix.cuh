@@ -34,6 +34,7 @@ namespace meteora {
 constexpr int kPfxKeys = kPrefixTile, kPfxRows = kPrefixRows;
 constexpr int kPfxThreads = 576;                     // warp 0: copies, warp 1: products, 16 warps of softmax
 constexpr int kPfxUnits = 16;                        // units described (more than the ring holds, so that copies seldom wait for a place)
+constexpr int kPfxOdd = 2 * kPfxUnits;               // units whose zeroed values are remembered (a group is at most kPfxUnits ahead of the other)
 constexpr int kPfxMasks = 16;                        // tiles whose page masks are remembered (more than the ring holds)
 
 template <int D> struct PrefixShape {
@@ -41,8 +42,8 @@ template <int D> struct PrefixShape {
     static constexpr int kStages = D == 128 ? 5 : 11;              // of keys or values of one tile
     static constexpr int kBarOff = (2 + kStages) * kTileBytes;     // barriers, then page masks, TMEM slot
     static constexpr int kBars = 2 * kStages + 19 + 2 * kPfxUnits;
-    static constexpr int kWords = kBarOff + kBars * 8;             // page masks [kPfxMasks], growth [16], zeroed [2 words], TMEM slot, then the units
-    static constexpr int kUnitOff = (kWords + (kPfxMasks + 19) * 4 + 15) / 16 * 16;
+    static constexpr int kWords = kBarOff + kBars * 8;             // page masks [kPfxMasks], growth [16], zeroed [kPfxOdd], TMEM slot, then the units
+    static constexpr int kUnitOff = (kWords + (kPfxMasks + kPfxOdd + 17) * 4 + 15) / 16 * 16;
     static constexpr int kSmem = 1024 + kUnitOff + kPfxUnits * 48;
 };
 
@@ -161,8 +162,8 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                    bar_ufree = bar_u + kPfxUnits * 8;
     volatile uint32_t* const s_mask = reinterpret_cast<volatile uint32_t*>(base_ptr + S::kWords);
     volatile uint32_t* const s_grow = s_mask + kPfxMasks;          // [tile of rows][half][quarter]
-    volatile uint32_t* const s_odd = s_grow + 16;                  // the unit in which values were zeroed, + 1
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kWords + (kPfxMasks + 18) * 4);
+    volatile uint32_t* const s_odd = s_grow + 16;                  // [unit of the share % kPfxOdd]: its id + 1, if values were zeroed in it
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + S::kWords + (kPfxMasks + kPfxOdd + 16) * 4);
     int4* const s_unit = reinterpret_cast<int4*>(base_ptr + S::kUnitOff);
     const int warp = warp_id(), lane = threadIdx.x & 31;
 
@@ -184,7 +185,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             mbar_init(bar_u + i * 8, 1);
             mbar_init(bar_ufree + i * 8, 17);
         }
-        *s_odd = 0;
+        for (int i = 0; i < kPfxOdd; ++i) s_odd[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -546,7 +547,11 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                             if ((w[q] & 0x7F80u) == 0x7F80u) w[q] &= 0xFFFF0000u, odd = true;
                             if ((w[q] & 0x7F800000u) == 0x7F800000u) w[q] &= 0xFFFFu, odd = true;
                         }
-                        if (odd) v[e] = x, *s_odd = (uint32_t)u.id + 1u;           // (the other tile of rows finds zeros)
+                        if (odd) {                                             // (the other tile of rows finds zeros: it sees the word before them)
+                            s_odd[(heard - 1) % kPfxOdd] = (uint32_t)u.id + 1u;
+                            __threadfence_block();
+                            v[e] = x;
+                        }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
@@ -586,7 +591,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
                 float o[kPart];
 #pragma unroll
                 for (int q = 0; q < kPart; q += 16) tmem_ld16(t_o + half * (D / 2) + c + q, *reinterpret_cast<float(*)[16]>(o + q));
-                if (kOwn && *s_odd == (uint32_t)u.id + 1u) {                 // what was zeroed, to the rows that see it
+                if (kOwn && s_odd[(heard - 1) % kPfxOdd] == (uint32_t)u.id + 1u) {     // what was zeroed, to the rows that see it
                     const PageList pages = page_list(p.batch, u.b);
                     const int from = max(u.tile0, lim_all / kPfxKeys) * kPfxKeys, to = min(lim, (u.tile0 + count) * kPfxKeys);
                     for (int key = from; key < to; ++key) {

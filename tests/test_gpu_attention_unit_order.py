@@ -41,3 +41,9 @@ def test_a_long_tile_before_forty_short_ones(D):
     """A bad value that only the long tiles' rows add by themselves: the second group is at that while more units than the ring
     describes pass by in which it has no rows."""
     check(80, 300, 40, D, [(100, 5, float("nan")), (101, D - 1, float("inf"))])
+
+
+@pytest.mark.parametrize("B,n,K,D", [(200, 300, 1, 128), (200, 300, 1, 64), (90, 380, 2, 128), (80, 300, 40, 64)])
+def test_bad_values_in_a_long_tile_and_in_the_short_one_behind_it(B, n, K, D):
+    """The first group finds the short tile's bad value while the second one still adds the long tile's."""
+    check(B, n, K, D, [(60, 7, float("nan")), (250, D - 1, float("-inf")), (270, 2, float("inf")), (n - 2, 11, float("nan"))])
