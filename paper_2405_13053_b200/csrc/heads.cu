@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) k_head_grad(const __grid_cons
             const float r = rsqrtf(fmaf(sq, p.inv_dim, p.eps));
             P rs, c;
             splat(rs, r);
-            splat(c, -r * r * r * (dot * p.inv_dim));
+            splat(c, -(r * (r * (r * (dot * p.inv_dim)))));           // (r^3 alone leaves fp32 where heads are small or large)
             E* dx = (E*)g.dx + away<VE>(t, g.dx_t) + away<VE>(h, g.dx_h);
 #pragma unroll
             for (int n = 0; n < NI; ++n) {
