@@ -351,7 +351,8 @@ int meteora_set_tuning(const char* name, int value);
  *
  * Conventions of these calls, next to those at the top of this file
  *   - Tensors of heads are x[T, heads, head_dim] with element strides of their own for tokens and heads (a slice of a
- *     fused q/k/v product needs no copy); the entries of a head are contiguous.  1 <= head_dim <= METEORA_MAX_HEAD_DIM.
+ *     fused q/k/v product needs no copy); the entries of a head are contiguous.  1 <= head_dim <= METEORA_MAX_HEAD_DIM,
+ *     T < 2^31 - 4096.
  *     Base pointers need the alignment of their element type; 16-byte aligned bases and strides take the wider loads.
  *   - An output may be its own input (same pointer and strides); any other overlap of tensors is out of contract, and
  *     an output whose strides make two of its entries coincide is refused.

@@ -8,6 +8,9 @@ namespace meteora {
 static bool known_dtype(meteora_dtype_t t) { return t == METEORA_F32 || t == METEORA_BF16; }
 static bool element_aligned(const void* p, meteora_dtype_t t) { return (uintptr_t)p % elem_size(t) == 0; }
 
+// Token counts stay so far below 2^31 that a launch may round them up to whole tiles or add a step to them.
+constexpr int kMostTokens = INT32_MAX - 4096;
+
 // A tensor x[T, heads, head_dim]; an output's entries must not coincide.
 static int check_heads(const meteora_heads_t* h, int T, int head_dim, meteora_dtype_t dtype, bool output) {
     if (!h || h->heads < 1 || h->stride_token < 0 || h->stride_head < 0) return METEORA_ERR_INVALID_ARG;
@@ -33,7 +36,7 @@ static int check_rotary(const meteora_rotary_t* rot, int head_dim) {
 
 static int check_sizes(int T, int head_dim, meteora_dtype_t dtype) {
     if (T < 0 || head_dim < 1 || !known_dtype(dtype)) return METEORA_ERR_INVALID_ARG;
-    return head_dim <= METEORA_MAX_HEAD_DIM ? METEORA_OK : METEORA_ERR_UNSUPPORTED_SHAPE;
+    return head_dim <= METEORA_MAX_HEAD_DIM && T <= kMostTokens ? METEORA_OK : METEORA_ERR_UNSUPPORTED_SHAPE;
 }
 
 static HeadRows rows_of(const meteora_heads_t& in, const meteora_heads_t& out, const void* gain) {
@@ -92,7 +95,7 @@ static int check_cache(const meteora_cache_t* c) {
 
 static int check_batch(const meteora_batch_t* b) {
     if (!b || b->B < 0 || b->T < 0 || b->table_width < 0 || b->prefix_len < 0) return METEORA_ERR_INVALID_ARG;
-    if (b->B > METEORA_MAX_BATCH) return METEORA_ERR_UNSUPPORTED_SHAPE;
+    if (b->B > METEORA_MAX_BATCH || b->T > kMostTokens) return METEORA_ERR_UNSUPPORTED_SHAPE;
     if (!b->cu_tokens && b->T != b->B) return METEORA_ERR_INVALID_ARG;
     if (b->T == 0 || b->B == 0) return METEORA_OK;
     if (!b->lengths || (b->table_width > 0 && !b->page_table)) return METEORA_ERR_INVALID_ARG;
@@ -166,7 +169,7 @@ int meteora_head_norm_rotary(const meteora_heads_t* q, const meteora_heads_t* k,
 }
 
 size_t meteora_head_norm_rotary_backward_workspace_bytes(int T, int q_heads, int k_heads, int head_dim) {
-    if (T < 0 || q_heads < 1 || k_heads < 0 || head_dim < 1 || head_dim > METEORA_MAX_HEAD_DIM || q_heads > 65535 || k_heads > 65535) return 0;
+    if (T < 0 || T > kMostTokens || q_heads < 1 || k_heads < 0 || head_dim < 1 || head_dim > METEORA_MAX_HEAD_DIM || q_heads > 65535 || k_heads > 65535) return 0;
     return head_grad_workspace_bytes(T, head_dim);
 }
 
