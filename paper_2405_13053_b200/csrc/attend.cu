@@ -103,8 +103,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join
             for (int c = 0; c < kParts; ++c) acc[c] = make_float4(acc[c].x * f0, acc[c].y * f0, acc[c].z * f0, acc[c].w * f0);
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
-                const float f = piece_factor(ml[a], base);
-                if (f == 0.f) continue;                              // (a piece in which the row sees nothing, or none; NaN goes on)
+                const float f = piece_factor(ml[a], base);           // (of 0 too: a value that is no number passes a weight next to nothing)
                 L = fmaf(f, ml[a].y, L);
 #pragma unroll
                 for (int c = 0; c < kParts; ++c) {
@@ -130,8 +129,8 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps) k_attend_join
             for (int c = 0; c < kParts; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int x = 0; x < kWarps; ++x) {
+                if (x >= n) continue;
                 const float f = piece_factor(s_ml[x], base);
-                if (f == 0.f) continue;
                 L = fmaf(f, s_ml[x].y, L);
 #pragma unroll
                 for (int c = 0; c < kParts; ++c) {

@@ -1,0 +1,33 @@
+"""Infinities and NaN in queries, keys and values of attention where the definition has an answer for them: against softmax in 64
+bits, which entries are finite.  Each of the kernels: one token (16 rows), a chunk (64), prompts on the tensor cores, fp32."""
+import numpy as np
+import pytest
+import torch
+
+from tests import heads_util as hu
+from tests.test_gpu_prefix_attention import BF16, F32, call, check, make
+
+pytestmark = pytest.mark.gpu
+SHAPES = {"tokens": dict(B=3, new=[1, 1, 1], held=[40, 3, 70], page=16, H=8, K=2, D=128, dtype=BF16), "chunk": dict(B=2, new=[9, 20], held=[40, 3], page=16, H=8, K=2, D=256, dtype=BF16),
+          "prompts": dict(B=2, new=[300, 40], held=[0, 70], page=16, H=4, K=2, D=64, dtype=BF16), "fp32": dict(B=2, new=[3, 1], held=[40, 70], page=16, H=4, K=2, D=64, dtype=F32)}
+
+
+@pytest.mark.parametrize("name", SHAPES)
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_a_value_that_is_no_number_under_a_weight_next_to_nothing(name, value):
+    """An own token's value where the prefix's keys have scores some 400 above: its weight is below 2^-500, and the average with
+    it is no finite number all the same."""
+    s = make(**SHAPES[name], prefix=100, nan=False)
+    s["q"][..., 0] = 16.0
+    s["kc"][..., 0] = 0.0
+    at = s["prefix_pages"].tolist()
+    s["kc"][at, :, :, 0] = 25.0 * s["q"].shape[2] ** 0.5
+    clean = call(s)
+    bad = dict(s, vc=s["vc"].clone())
+    for b in range(len(s["lengths"])):                               # the sequences' first own token
+        bad["vc"][int(s["table"][b, 0]), :, 0, 3] = value
+    y, lse = call(bad, return_lse=True)
+    assert torch.isfinite(lse).all() and torch.isfinite(clean).all()
+    assert not torch.isfinite(y[..., 3]).any()
+    rest = torch.arange(y.shape[2], device="cuda") != 3
+    assert torch.equal(y[..., rest], clean[..., rest])
