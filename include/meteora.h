@@ -491,7 +491,8 @@ int meteora_cache_append(const meteora_heads_t* k, const meteora_heads_t* v, con
  * prefix and the own tokens up to its own (i <= lengths[b] + j), query head h reading kv head h / (q heads / kv heads).
  * The prefix is computed once for the rows of all sequences together; each sequence's own pages for its own rows.
  *   q, out     [T, q_heads, head_dim] in the cache's dtype; q_heads a multiple of kv_heads.  A row that sees no key at
- *              all (every page dropped) is zero.  Rows of tokens without a sequence are left as they were.
+ *              all (every page dropped) is zero; one that sees scores of -inf alone is NaN (0 / 0).  Rows of tokens without a
+ *              sequence are left as they were.
  *   lse        optional fp32 [T, q_heads]: logarithm of the row's sum of exp(scale * q . k), -inf for a row that sees none.
  *   workspace  meteora_prefix_attention_workspace_bytes(...) bytes (sizes of cache and batch are read, no pointers), 16-byte
  *              aligned, its header zeroed once (meteora_workspace_init); meteora_workspace_status reads its status word.

@@ -31,3 +31,28 @@ def test_a_value_that_is_no_number_under_a_weight_next_to_nothing(name, value):
     assert not torch.isfinite(y[..., 3]).any()
     rest = torch.arange(y.shape[2], device="cuda") != 3
     assert torch.equal(y[..., rest], clean[..., rest])
+
+
+@pytest.mark.parametrize("name", SHAPES)
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_scores_that_are_all_minus_infinity(name, prefix):
+    """Keys of -inf in one entry under queries above 0 there: softmax over scores of -inf alone is 0 / 0.  Other heads stay, and a row
+    whose pages are all gone is still zero."""
+    s = make(**SHAPES[name], prefix=prefix, nan=False, seed=2)
+    gone, H, K = len(s["lengths"]) - 1, s["q"].shape[1], s["kc"].shape[1]
+    s["table"][gone] = -1                                            # the last sequence has its prefix alone
+    clean = call(s)
+    bad = dict(s, kc=s["kc"].clone(), q=s["q"].clone())
+    bad["q"][:, :H // K, 5] = 0.5
+    bad["kc"][:, 0, :, 5] = float("-inf")
+    y, lse = call(bad, return_lse=True)
+    assert torch.equal(y[:, H // K:], clean[:, H // K:]) and torch.isfinite(lse[:, H // K:]).all() == (prefix > 0)
+    seen = torch.tensor([prefix > 0 or hu.places(dict(cu=None if s["cu"] is None else s["cu"].tolist(), lengths=s["lengths"].tolist()), t)[0] != gone
+                         for t in range(y.shape[0])], device="cuda")
+    assert torch.isnan(y[seen, :H // K]).all() and (y[~seen] == 0).all() and (lse[:, :H // K] == -float("inf")).all()
+    part = dict(bad, kc=bad["kc"].clone())                           # one key of the first sequence with a score of its own
+    part["kc"][int(s["table"][0, 0]), 0, 0] = 0.0
+    y = call(part)
+    v = s["vc"][int(s["table"][0, 0]), 0, 0]
+    first = int(s["cu"][1]) if s["cu"] is not None else 1
+    assert torch.equal(y[:first, :H // K], v.expand(first, H // K, -1))
