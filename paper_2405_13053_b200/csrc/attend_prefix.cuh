@@ -50,8 +50,8 @@ template <int D> struct PrefixShape {
 struct PrefixTcParams {
     AttendParams a;
     int box_rows, box_shift;                         // keys per copy: divides the page and the tile
-    int sign;                                        // of the scale: the queries are multiplied by it, scale_log2 is above 0 (a masked
-                                                     // score, -inf, stays one)
+    int sign;                                        // of the scale (-1, 0, 1): the queries are multiplied by it, scale_log2 is above 0 (a
+                                                     // masked score, -inf, stays one)
 };
 
 // A_i P^T: A from TMEM, B from shared memory.
@@ -112,6 +112,11 @@ __device__ __forceinline__ unsigned long long fma2_of(unsigned long long a, unsi
     unsigned long long r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
+}
+
+// Two bf16 times 0: NaN where one is no finite number.
+__device__ __forceinline__ uint32_t times_zero(uint32_t v) {
+    return ((v & 0x7F80u) == 0x7F80u ? 0x7FFFu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0x7FFF0000u : 0u);
 }
 
 // The units of a CTA's share, one after the other; the copies' warp walks them and leaves each one's description.
@@ -413,7 +418,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
             // queries: a warp 16 of the 32 rows, each row's chunks by neighbouring lanes
             {
                 constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks;
-                const uint32_t flip = pp.sign < 0 ? 0x80008000u : 0u, keep = pp.sign ? 0xFFFFFFFFu : 0u;
+                const uint32_t flip = pp.sign < 0 ? 0x80008000u : 0u;
                 const int c = lane % kChunks;
                 uint4 v[16 / kAtOnce];
 #pragma unroll
@@ -436,7 +441,8 @@ k_attend_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUt
 #pragma unroll
                 for (int q = 0; q < 16 / kAtOnce; ++q) {
                     const int rr = quad * 32 + half * 16 + q * kAtOnce + lane / kChunks;
-                    v[q].x = (v[q].x ^ flip) & keep, v[q].y = (v[q].y ^ flip) & keep, v[q].z = (v[q].z ^ flip) & keep, v[q].w = (v[q].w ^ flip) & keep;
+                    if (pp.sign == 0) v[q] = make_uint4(times_zero(v[q].x), times_zero(v[q].y), times_zero(v[q].z), times_zero(v[q].w));
+                    v[q].x ^= flip, v[q].y ^= flip, v[q].z ^= flip, v[q].w ^= flip;
                     *reinterpret_cast<uint4*>(base_ptr + i * S::kTileBytes + (c >> 3) * (kPfxKeys * 128) + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[q];
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -56,3 +56,27 @@ def test_scores_that_are_all_minus_infinity(name, prefix):
     v = s["vc"][int(s["table"][0, 0]), 0, 0]
     first = int(s["cu"][1]) if s["cu"] is not None else 1
     assert torch.equal(y[:first, :H // K], v.expand(first, H // K, -1))
+
+
+@pytest.mark.parametrize("name", SHAPES)
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("prefix", [0, 200])
+def test_no_numbers_under_a_scale_of_zero(name, value, prefix):
+    """scale = 0 makes every score 0 and the row an average of what it sees; a query or a key that is no finite number makes its
+    scores NaN, 0 times it, and the rows with it."""
+    s = make(**SHAPES[name], prefix=prefix, nan=False, seed=3)
+    clean, lse = call(s, scale=0.0, return_lse=True)
+    check(s, clean, lse, scale=0.0)
+    t, h, H, K = s["q"].shape[0] - 1, 1, s["q"].shape[1], s["kc"].shape[1]
+    bad = dict(s, q=s["q"].clone())
+    bad["q"][t, h, 9] = value
+    y = call(bad, scale=0.0)
+    hit = torch.zeros(y.shape[:2], dtype=torch.bool, device="cuda")
+    hit[t, h] = True
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit])
+    bad = dict(s, kc=s["kc"].clone())
+    bad["kc"][int(s["table"][0, 0]), 0, 0, 9] = value                # seen by the first sequence, through one kv head
+    y = call(bad, scale=0.0)
+    hit[:] = False
+    hit[:int(s["cu"][1]), :H // K] = True
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit])
