@@ -347,16 +347,21 @@ def meteora_cache_append(k, v, k_cache, v_cache, page_table, lengths, rot: Optio
                                                     q_gain, k_gain, eps, out_q)
 
 
-def meteora_prefix_attention_workspace(q, k_cache, page_table, prefix_len: int = 0) -> torch.Tensor:
-    """Scratch for meteora_prefix_attention calls of these sizes (header zeroed); one per stream."""
+def meteora_prefix_attention_workspace_bytes(q, k_cache, page_table, prefix_len: int = 0) -> int:
+    """Bytes that meteora_prefix_attention calls of these sizes need (only shapes and types are read).  A larger workspace serves as well."""
     T, H, _ = q.shape
     n, kv, page, D = k_cache.shape
     cache = MeteoraCache(None, None, n, kv, page, D, _dtype_code(k_cache))
     batch = MeteoraBatch(page_table.shape[0], T, None, None, None, page_table.shape[1], prefix_len, None)
-    n = load_library().meteora_prefix_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), H)
-    if n == 0:
+    need = load_library().meteora_prefix_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), H)
+    if need == 0:
         raise MeteoraError(-1, "meteora_prefix_attention_workspace_bytes")
-    ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+    return need
+
+
+def meteora_prefix_attention_workspace(q, k_cache, page_table, prefix_len: int = 0) -> torch.Tensor:
+    """Scratch for meteora_prefix_attention calls of these sizes (header zeroed); one per stream."""
+    ws = torch.empty(meteora_prefix_attention_workspace_bytes(q, k_cache, page_table, prefix_len), dtype=torch.uint8, device=q.device)
     ws[:4096].zero_()
     return ws
 

@@ -106,12 +106,46 @@ class FixedLinears:
         return [self.out[n] for n in names]
 
 
+class AttentionScratch:
+    """The workspace of attention calls that follow one another, on one stream or on streams that wait for each other: one
+    buffer, as large as the largest call so far has needed.  One that a captured graph uses is kept when it is outgrown; a call
+    that is captured before any of its size has run takes memory of the graph's own, which goes with the graph."""
+
+    def __init__(self):
+        from . import binding
+        self.mb = binding
+        self.buffers: Dict[int, torch.Tensor] = {}      # by size: the largest is in use
+        self.captured = set()                           # sizes that graphs hold on to
+
+    def of(self, q: torch.Tensor, k: torch.Tensor, page_table: torch.Tensor, prefix_len: int) -> torch.Tensor:
+        need, size = self.mb.meteora_prefix_attention_workspace_bytes(q, k, page_table, prefix_len), max(self.buffers, default=0)
+        with torch.cuda.device(q.device):
+            capturing = torch.cuda.is_current_stream_capturing()
+            if need > size:
+                made = self.mb.meteora_prefix_attention_workspace(q, k, page_table, prefix_len)
+                if capturing:
+                    return made
+                if size and size not in self.captured:  # (its memory waits for the calls that are under way)
+                    self.buffers.pop(size).record_stream(torch.cuda.current_stream())
+                self.buffers[need] = made
+                return made
+        if capturing:
+            self.captured.add(size)
+        return self.buffers[size]
+
+    def status(self) -> int:
+        """0, or METEORA_ERR_TIMEOUT where a wait of a call has run out (synchronises)."""
+        return min([self.mb.meteora_workspace_status(ws) for ws in self.buffers.values()] or [0])
+
+
 class PagedCache:
     """One layer's keys and values of B sequences of up to `tokens` own tokens each, in pages, behind a prefix of `prefix_len`
     tokens that all of them share.  `lengths` are the sequences' own tokens in the cache: a step appends at them and
-    attends, `advance` moves them on afterwards (tensors on the device: a captured step goes on as they grow)."""
+    attends, `advance` moves them on afterwards (tensors on the device: a captured step goes on as they grow).  Steps of one
+    cache follow one another.  Layers that do so too may share their `scratch`."""
 
-    def __init__(self, B: int, tokens: int, prefix_len: int = 0, page_size: int = 64, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, B: int, tokens: int, prefix_len: int = 0, page_size: int = 64, dtype=torch.bfloat16, device="cuda",
+                 scratch: Optional[AttentionScratch] = None):
         from . import binding
         self.mb, self.prefix_len = binding, prefix_len
         width, n_prefix = -(-tokens // page_size), -(-prefix_len // page_size)
@@ -121,7 +155,11 @@ class PagedCache:
         self.page_table, self.prefix_pages = pages[:B * width].view(B, width), pages[B * width:]
         self.lengths = torch.zeros(B, dtype=torch.int32, device=device)
         self.rot = binding.meteora_rotary_init(HEAD_DIM, ROPE_THETA)
-        self.workspaces: Dict[int, torch.Tensor] = {}
+        self.scratch = AttentionScratch() if scratch is None else scratch
+
+    @property
+    def workspaces(self) -> Dict[int, torch.Tensor]:
+        return self.scratch.buffers
 
     def append_prefix(self, k: torch.Tensor, v: torch.Tensor) -> None:
         """Keys (not yet rotated) and values [prefix_len, N_KV_HEADS, HEAD_DIM] of the prefix."""
@@ -131,17 +169,18 @@ class PagedCache:
 
     def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_tokens: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Appends the new tokens' k (rotated) and v [T, N_KV_HEADS, HEAD_DIM] and returns the attention of their q."""
-        T = q.shape[0]
         q = self.mb.meteora_cache_append(k, v, self.k, self.v, self.page_table, self.lengths, self.rot, cu_tokens=cu_tokens,
                                          prefix_len=self.prefix_len, q=q)
-        if T not in self.workspaces:            # made on first use, so that a CUDA graph can be captured afterwards
-            self.workspaces[T] = self.mb.meteora_prefix_attention_workspace(q, self.k, self.page_table, self.prefix_len)
         return self.mb.meteora_prefix_attention(q, self.k, self.v, self.page_table, self.lengths, self.prefix_pages, self.prefix_len,
-                                                cu_tokens=cu_tokens, workspace=self.workspaces[T])
+                                                cu_tokens=cu_tokens, workspace=self.scratch.of(q, self.k, self.page_table, self.prefix_len))
 
     def advance(self, new) -> None:
         """`new`: tokens of the step per sequence (a number, or int32 [B])."""
         self.lengths += new
+
+    def status(self) -> int:
+        """0, or METEORA_ERR_TIMEOUT where a wait of an attention call has run out (synchronises)."""
+        return self.scratch.status()
 
 
 def layer_forward(x: torch.Tensor, norms: Dict[str, torch.Tensor], linears, positions: Optional[torch.Tensor] = None,
