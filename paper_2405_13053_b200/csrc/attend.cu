@@ -258,8 +258,8 @@ static AttendPlan plan_attend(const AttendSizes& z, void* workspace) {
         if (p.tc) {
             set_tc(p.prefix);
             p.prefix.total = (int)(prefix_units * ((z.prefix_len + kPrefixTile - 1) / kPrefixTile));
-            // (two tiles each at least: 64 rows of 32 heads over 2048 keys, with 64 sequences' own tokens and the join, 44.9 us; one
-            // each, 16 pieces for a row instead of 8, 48.5; four 46.3)
+            // (two tiles each at least: 64 rows of 32 heads over 2048 keys, with 64 sequences' own tokens and the join, 44.8 us; one
+            // each, 16 pieces for a row instead of 8, 49.3; four 49.4)
             p.prefix.workers = std::max(1, std::min(148, p.prefix.total >> 1));
         } else {
             set_kernel(p.prefix, z, plan.mma);

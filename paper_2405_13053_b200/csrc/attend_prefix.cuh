@@ -14,7 +14,7 @@
 // rows tensor core and exponentials are nearly even.  Measured, heads of 128: 512 rows of 8 kv heads over 32768 keys (69 GFLOP)
 // 84 us, 880 rows of 40 heads over 8192 keys (148 GFLOP) 171 us = 0.86 PFLOP/s.  With the softmax left out (wrong results) the
 // copies and products alone are 57 and 122 us, twice the products' cycles: every 256 rows read their 64 KB of a tile
-// through L2, 5.5 TB/s over all SMs, and that bounds this form; a pair of SMs with 512 rows would halve it.  Slower or even:
+// through L2, 5.9 TB/s over all SMs (1013 MB in the 171 us), and that bounds this form; a pair of SMs with 512 rows would halve it.  Slower or even:
 // maxima exchanged a tile later and a polynomial for a part of the exponentials 87 us (of 82); one thread per row, 8 warps
 // of softmax instead of 16, within 5%.
 // A row's reference m is not its running maximum: it stays until the maximum is 8 above it, which leaves weights below 2^8

@@ -8,7 +8,7 @@
 // through registers, half as many, 20.5 us for 4096 tokens of 32 + 8 heads of 128), the first asked for before the angles.  Few
 // tokens: one per CTA, its rows dealt over several CTAs.
 // Every entry is read once and written once: 84 MB there, 15.5 us = 5.4 TB/s for the rotation.  With the norm instructions bound
-// it (350 for a warp's four rows, 0.7 issued per scheduler and cycle): 19.9 us; gains and places kept in registers from row to
+// it (361 for a warp's four rows, 0.66 issued per scheduler and cycle): 19.9 us; gains and places kept in registers from row to
 // row save a fifth of them and cost the fourth CTA of an SM or spills, 22 to 32 us.
 #include <algorithm>
 
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kHeadThreads, NI > 1 ? 2 : 4) k_head_pass(cons
 // and k_gain_sums adds those up in their order.  With u = dn * x and c = r^3 mean(gain * u):
 //     dgain += r u,   dx = (gain r) dn - c x.
 // x and dy are read once, dx written once: 126 MB for 4096 tokens of 32 + 8 heads of 128, 30.5 us = 4.1 TB/s.  Bound by
-// instructions (450 for a warp's four rows) that 16 warps of an SM, at 124 registers a thread, issue at 0.55 per scheduler and
+// instructions (481 for a warp's four rows) that 15 warps of an SM, at 128 registers a thread, issue at 0.55 per scheduler and
 // cycle.  Slower: rows of one token after the other in a group, its angles in registers, 35.5 us.
 constexpr int kGradTokens = 16;
 
