@@ -115,23 +115,30 @@ class AttentionScratch:
         from . import binding
         self.mb = binding
         self.buffers: Dict[int, torch.Tensor] = {}      # by size: the largest is in use
+        self.size = 0                                   # of that one
         self.captured = set()                           # sizes that graphs hold on to
+        self.needs: Dict[tuple, int] = {}               # bytes by shapes
 
     def of(self, q: torch.Tensor, k: torch.Tensor, page_table: torch.Tensor, prefix_len: int) -> torch.Tensor:
-        need, size = self.mb.meteora_prefix_attention_workspace_bytes(q, k, page_table, prefix_len), max(self.buffers, default=0)
-        with torch.cuda.device(q.device):
-            capturing = torch.cuda.is_current_stream_capturing()
-            if need > size:
-                made = self.mb.meteora_prefix_attention_workspace(q, k, page_table, prefix_len)
-                if capturing:
-                    return made
-                if size and size not in self.captured:  # (its memory waits for the calls that are under way)
-                    self.buffers.pop(size).record_stream(torch.cuda.current_stream())
-                self.buffers[need] = made
+        if q.device.index != torch.cuda.current_device():
+            with torch.cuda.device(q.device):
+                return self.of(q, k, page_table, prefix_len)
+        shapes = (q.shape, k.shape, k.dtype, page_table.shape, prefix_len)
+        need = self.needs.get(shapes)
+        if need is None:
+            need = self.needs[shapes] = self.mb.meteora_prefix_attention_workspace_bytes(q, k, page_table, prefix_len)
+        capturing = torch.cuda.is_current_stream_capturing()
+        if need > self.size:
+            made = self.mb.meteora_prefix_attention_workspace(q, k, page_table, prefix_len)
+            if capturing:
                 return made
+            if self.size and self.size not in self.captured:      # (its memory waits for the calls that are under way)
+                self.buffers.pop(self.size).record_stream(torch.cuda.current_stream())
+            self.buffers[need], self.size = made, need
+            return made
         if capturing:
-            self.captured.add(size)
-        return self.buffers[size]
+            self.captured.add(self.size)
+        return self.buffers[self.size]
 
     def status(self) -> int:
         """0, or METEORA_ERR_TIMEOUT where a wait of a call has run out (synchronises)."""
